@@ -18,6 +18,8 @@
  *   fsharp_kernel_apply   the unnormalised operator Khat^(alpha) C (softmax and Gaussian kernels)
  *   fsharp_attend_key_state, fsharp_attend_with_state   the same Y with the keys of a sequence spread over
  *                         several calls or devices (key-side sums of disjoint key ranges add)
+ *   fsharp_rotate         rotary positions on queries and keys, and their gradient
+ *   fsharp_cross_attend, fsharp_cross_attend_backward   exact softmax attention to states of another length
  *
  * Conventions common to every call
  *   - All data pointers are DEVICE pointers owned by the caller unless the
@@ -112,7 +114,7 @@ int64_t fsharp_launch_count(const fsharp_ctx* ctx);
  * between two reads).  fsharp_read_timing synchronises the stream and returns, for
  * kernel ids 0..cap-1, the summed milliseconds and the launch count since the last
  * read (host arrays of `cap` entries); fsharp_kernel_name maps an id to the kernel's
- * name ("" for unused ids).  Ids are below 32. */
+ * name ("" for unused ids).  Ids are below 64. */
 int fsharp_set_timing(fsharp_ctx* ctx, int on);
 int fsharp_read_timing(fsharp_ctx* ctx, int cap, float* total_ms, int* launches);
 const char* fsharp_kernel_name(int id);
@@ -267,6 +269,78 @@ int fsharp_attend_with_state(fsharp_ctx* ctx, const void* Q, const void* K, cons
 int fsharp_kernel_apply(fsharp_ctx* ctx, const void* X, const void* Y, const void* C, const float* Omega,
                         const double* params, double alpha, const fsharp_dims* dims, int dtype, float qk_scale,
                         void* out);
+
+/* Rotary positions (no counterpart in the paper: what a decoder layer does to queries and keys before fsharp_stats,
+ * fsharp_attend and the rest see them).  Pair j < rot / 2 of a head is (x[j], x[j + rot/2]) in the HALF layout and
+ * (x[2j], x[2j + 1]) in the INTERLEAVED one; at position p
+ *   (a, b) -> gain (a cos t - b sin t, b cos t + a sin t),   t = p theta_j,   theta_j = base^(-2j / rot)
+ * and features from rot on pass through unchanged.  Frequencies for contexts beyond the trained one:
+ *   LINEAR  theta_j / factor
+ *   NTK     base factor^(rot / (rot - 2)) in place of base (rot > 2)
+ *   PARTS   theta_j (keep + (1 - keep) / factor), keep = clamp((n - slow) / (fast - slow), 0, 1) with
+ *           n = original theta_j / 2 pi the pair's turns in the trained length `original`
+ * transpose != 0 applies the transposed map (t -> -t, gain kept): the gradient of the call, dX from dY.
+ * Angles are formed in 64 bits (positions up to 2^31 in magnitude keep fp32's accuracy); each output is rounded once.
+ * Q [B,H,L,d] and K [B,Hk,L,d] are turned by one launch (Hk = 0: queries alone, K and Kout may be NULL).
+ * pos: device int64, position of token i of sequence b at pos[b * pos_stride + i] (pos_stride 0: shared by the batch);
+ * NULL means i.  pos0 is added either way.  d in {16, 32, 64, 128}, rot even, 2 <= rot <= d.
+ * Qout may be Q and Kout may be K (the same pointer and strides); outputs that overlap anything else are undefined. */
+enum { FSHARP_ROT_HALF = 0, FSHARP_ROT_INTERLEAVED = 1 };
+enum { FSHARP_ROPE_PLAIN = 0, FSHARP_ROPE_LINEAR = 1, FSHARP_ROPE_NTK = 2, FSHARP_ROPE_PARTS = 3 };
+typedef struct {
+  int32_t rot, layout, scaling, reserved;
+  double base, factor, original, slow, fast, gain;    /* factor: not PLAIN; original, slow, fast: PARTS */
+} fsharp_rope;
+typedef struct {
+  int32_t B, L, H, Hk, d;
+  int64_t q_stride[3], k_stride[3];     /* element strides (batch, head, token) of Q, K */
+  int64_t qo_stride[3], ko_stride[3];   /* of Qout, Kout */
+} fsharp_rotate_dims;
+int fsharp_rotate(fsharp_ctx* ctx, const void* Q, const void* K, const int64_t* pos, int64_t pos_stride, int64_t pos0,
+                  const fsharp_rope* rope, const fsharp_rotate_dims* dims, int dtype, int transpose, void* Qout,
+                  void* Kout);
+
+/* Exact softmax cross attention to an encoder's states of another length (no counterpart in the paper, whose random
+ * features pay when there are many more keys than features; a decoder that looks at a short or moderate encoding, and
+ * one that reads it token by token, takes the exact form):
+ *   S_ij = scale Q_i . K_j over the keys j that sequence b has,  P = softmax_j S,  Y_i = sum_j P_ij V_j,
+ *   lse_i = log sum_j exp S_ij.
+ * Q [B,H,Lq,d], K [B,Hk,Lk,d], V [B,Hk,Lk,dv], Y [B,H,Lq,dv] of type `dtype`; H a multiple of Hk, query head h reads
+ * key head h / (H / Hk).  d, dv in {16, 32, 64, 128}, any Lq and Lk (Lq = 1: a decoding step), scale >= 0.
+ * key_len: device int32 [B], the keys of sequence b are 0 .. key_len[b] - 1 (values are clamped to 0 .. Lk); NULL: all Lk.
+ * key_mask: device bytes, key j of sequence b is seen where key_mask[b * mask_stride + j] is not zero (mask_stride 0:
+ * one mask for the batch); NULL: all.  Both may be given.  What K and V hold at keys that are not seen, NaNs and
+ * infinities too, changes nothing.  A row that sees no key, or only scores of minus infinity, has Y = 0 and lse = -inf
+ * (Lk = 0 is allowed).  lse: float32, dense [B,H,Lq], or NULL.
+ *
+ * fsharp_cross_attend_backward writes, for a cotangent dY of Y, with D_i = dY_i . Y_i and dS = scale P (dY V^T - D):
+ *   dQ = dS K,  dK = dS^T Q,  dV = P^T dY  (summed over the query heads that share a key head),
+ * zero for rows that see nothing and for keys that are not seen.  Y and lse are those of the forward call.  All sums
+ * are made in a fixed order: the same call gives the same bits.
+ *
+ * scratch: device memory of at least fsharp_cross_scratch_bytes() bytes (16-byte aligned; may be NULL where that is 0),
+ * used while the call's work is on the stream and not read before it is written.  It is the caller's, not the context's,
+ * so that captured graphs and calls on several streams can each have their own; a graph keeps the pointer.
+ * bf16 runs on the tensor cores (fewer than FSHARP_CROSS_FEW_ROWS query rows per key head: multiply-add kernels that
+ * stream K and V), fp32 on the multiply-add pipe in fp32 throughout.  FSHARP_IMPL_SIMT forces the multiply-add kernels;
+ * FSHARP_IMPL_TENSOR refuses fp32 (FSHARP_E_SHAPE).  B * Hk <= 65535. */
+#define FSHARP_CROSS_FEW_ROWS 5
+typedef struct {
+  int32_t B, H, Hk, Lq, Lk, d, dv;
+  int64_t q_stride[3], k_stride[3], v_stride[3], y_stride[3];         /* element strides (batch, head, token) */
+  int64_t dy_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];     /* the backward pass alone */
+  int64_t mask_stride;
+} fsharp_cross_dims;
+/* Bytes of scratch of the forward (backward = 0) or backward call, or a negative error code.  They depend on sizes and
+ * on the context's device and kernel family alone. */
+int64_t fsharp_cross_scratch_bytes(const fsharp_ctx* ctx, const fsharp_cross_dims* dims, int dtype, int backward);
+int fsharp_cross_attend(fsharp_ctx* ctx, const void* Q, const void* K, const void* V, const int32_t* key_len,
+                        const uint8_t* key_mask, const fsharp_cross_dims* dims, int dtype, float scale, void* Y, float* lse,
+                        void* scratch, int64_t scratch_bytes);
+int fsharp_cross_attend_backward(fsharp_ctx* ctx, const void* Q, const void* K, const void* V, const void* Y,
+                                 const float* lse, const void* dY, const int32_t* key_len, const uint8_t* key_mask,
+                                 const fsharp_cross_dims* dims, int dtype, float scale, void* dQ, void* dK, void* dV,
+                                 void* scratch, int64_t scratch_bytes);
 
 /* The whole path on HOST buffers: copies Q, K, V (dense [B,H,L,*], type `dtype`)
  * to the device, runs stats -> fit -> attend, copies Y back and waits for it.

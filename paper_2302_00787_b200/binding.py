@@ -26,7 +26,8 @@ EXPORTS = [
     "fsharp_forward_host", "fsharp_pair_estimate", "fsharp_set_timing", "fsharp_read_timing",
     "fsharp_kernel_name", "fsharp_static_scratch_bytes", "fsharp_featurize_static", "fsharp_kernel_apply",
     "fsharp_key_state_splits", "fsharp_attend_key_state", "fsharp_attend_with_state", "fsharp_attend_backward",
-    "fsharp_selftest_bounded_wait",
+    "fsharp_selftest_bounded_wait", "fsharp_rotate", "fsharp_cross_scratch_bytes", "fsharp_cross_attend",
+    "fsharp_cross_attend_backward",
 ]
 
 
@@ -42,6 +43,28 @@ class fsharp_dims(C.Structure):
                 ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
                 ("v_stride", C.c_int64 * 3), ("y_stride", C.c_int64 * 3),
                 ("omega_head_stride", C.c_int64)]
+
+
+ROT_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
+
+
+class fsharp_rope(C.Structure):
+    _fields_ = [("rot", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("reserved", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("original", C.c_double), ("slow", C.c_double),
+                ("fast", C.c_double), ("gain", C.c_double)]
+
+
+class fsharp_rotate_dims(C.Structure):
+    _fields_ = [("B", C.c_int32), ("L", C.c_int32), ("H", C.c_int32), ("Hk", C.c_int32), ("d", C.c_int32),
+                ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
+                ("qo_stride", C.c_int64 * 3), ("ko_stride", C.c_int64 * 3)]
+
+
+class fsharp_cross_dims(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("B", "H", "Hk", "Lq", "Lk", "d", "dv")]
+                + [(n + "_stride", C.c_int64 * 3) for n in ("q", "k", "v", "y", "dy", "dq", "dk", "dv")]
+                + [("mask_stride", C.c_int64)])
 
 
 _lib = None
@@ -81,6 +104,12 @@ def load_library() -> C.CDLL:
         "fsharp_attend_with_state": (i32, [vp, vp, vp, vp, vp, vp, dims_p, i32, i32, f32, vp, vp, i32, vp]),
         "fsharp_forward_host": (i32, [vp, vp, vp, vp, vp, dims_p, i32, i32, i32, i32, f32, vp]),
         "fsharp_pair_estimate": (i32, [vp, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp]),
+        "fsharp_rotate": (i32, [vp, vp, vp, vp, i64, i64, C.POINTER(fsharp_rope), C.POINTER(fsharp_rotate_dims), i32, i32, vp,
+                                vp]),
+        "fsharp_cross_scratch_bytes": (i64, [vp, C.POINTER(fsharp_cross_dims), i32, i32]),
+        "fsharp_cross_attend": (i32, [vp, vp, vp, vp, vp, vp, C.POINTER(fsharp_cross_dims), i32, f32, vp, vp, vp, i64]),
+        "fsharp_cross_attend_backward": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, vp, C.POINTER(fsharp_cross_dims), i32, f32, vp,
+                                               vp, vp, vp, i64]),
         "fsharp_set_timing": (i32, [vp, i32]),
         "fsharp_selftest_bounded_wait": (i32, [vp, i32]),
         "fsharp_read_timing": (i32, [vp, i32, C.POINTER(C.c_float), C.POINTER(i32)]),
@@ -128,6 +157,32 @@ def _strides(t: torch.Tensor):
     return (C.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
 
 
+def _readable(t: torch.Tensor) -> torch.Tensor:
+    """`t`, or a dense copy where its strides cannot be told to the library: a tensor broadcast along every dimension
+    (three zeros mean dense there), rows or a start that are not 16-byte aligned, a last dimension with gaps."""
+    if t.dim() != 4:
+        raise ValueError("expected a [B, H, L, inner] tensor")
+    es = t.element_size()
+    strides = [s for s, n in zip(t.stride()[:3], t.shape[:3]) if n > 1]
+    if (t.shape[3] > 1 and t.stride(3) != 1) or (strides and not any(strides)) or any(s * es % 16 for s in strides) \
+            or t.data_ptr() % 16:
+        return t.contiguous() if not t.is_contiguous() else t.clone()
+    return t
+
+
+def _free_strides(t: torch.Tensor):
+    """_strides with those of dimensions of size one, which nothing reads, as a dense tensor has them."""
+    B, H, L, inner = t.shape
+    dense = (H * L * inner, L * inner, inner)
+    return (C.c_int64 * 3)(*(s if n > 1 else z for s, n, z in zip(t.stride()[:3], (B, H, L), dense)))
+
+
+def _check_written(name: str, t: torch.Tensor) -> None:
+    """Refuses an output that holds one place for several values."""
+    if any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
+        raise ValueError(f"{name}: a broadcast tensor cannot be written")
+
+
 def make_dims(B, H, Lq, Lk, d, dv, M, pool=POOL_PER_BH, q=None, k=None, v=None, y=None,
               omega_head_stride=0) -> fsharp_dims:
     dm = fsharp_dims()
@@ -137,6 +192,15 @@ def make_dims(B, H, Lq, Lk, d, dv, M, pool=POOL_PER_BH, q=None, k=None, v=None, 
             setattr(dm, name, _strides(t))
     dm.omega_head_stride = omega_head_stride
     return dm
+
+
+def make_rope(rot, layout="half", base=10000.0, scaling="none", factor=1.0, original=0, slow=1.0, fast=32.0,
+              gain=1.0) -> fsharp_rope:
+    """Rotary positions of the first `rot` features of a head; the fields as in fsharp.h."""
+    r = fsharp_rope()
+    r.rot, r.layout, r.scaling = rot, ROT_LAYOUTS[layout], ROPE_SCALINGS[scaling]
+    r.base, r.factor, r.original, r.slow, r.fast, r.gain = base, factor, original, slow, fast, gain
+    return r
 
 
 class Context:
@@ -188,7 +252,7 @@ class Context:
 
     def read_timing(self) -> dict:
         """{kernel name: (total milliseconds, launches)} since the last read."""
-        cap = 32
+        cap = 64
         ms = (C.c_float * cap)()
         n = (C.c_int * cap)()
         _check(self.lib.fsharp_read_timing(self._h, cap, ms, n), "fsharp_read_timing")
@@ -318,6 +382,119 @@ class Context:
                                             params.data_ptr(), float(alpha), C.byref(dm), _dtype_code(X), qk_scale,
                                             out.data_ptr()), "fsharp_kernel_apply")
         return out
+
+    def _mine(self, *named):
+        """Refuses tensors that are not on this context's device: the library reads through their pointers unchecked."""
+        for name, t in named:
+            if t is not None and (t.device.type != "cuda" or t.device.index != self.device):
+                raise ValueError(f"{name}: expected a tensor on cuda:{self.device}, got {t.device}")
+
+    def fsharp_rotate(self, Q, K, rope, pos=None, pos0=0, transpose=False, out=None):
+        """Rotary positions (make_rope) on Q [B,H,L,d] and K [B,Hk,L,d] (K may be None): (Q', K').  pos: int64 [B,L] or
+        [L], None for 0 .. L-1; pos0 is added to it.  transpose: the gradient.  out: a pair of tensors to write, Q and K
+        themselves among them; the default is new dense ones."""
+        self._mine(("Q", Q), ("K", K), ("pos", pos))
+        Q, K = _readable(Q), None if K is None else _readable(K)
+        B, H, L, d = Q.shape
+        if K is not None and (K.dim() != 4 or K.shape[0] != B or K.shape[2:] != Q.shape[2:] or K.dtype != Q.dtype):
+            raise ValueError(f"K: expected {(B, 'Hk', L, d)} of {Q.dtype}, got {tuple(K.shape)} of {K.dtype}")
+        if pos is not None and (pos.dtype != torch.int64 or tuple(pos.shape) not in ((B, L), (L,))
+                                or (L > 1 and pos.stride(-1) != 1)):
+            raise ValueError("pos: expected int64 [B, L] or [L] whose last dimension is contiguous")
+        if out is None:
+            out = (torch.empty(Q.shape, dtype=Q.dtype, device=Q.device),
+                   None if K is None else torch.empty(K.shape, dtype=K.dtype, device=K.device))
+        dm = fsharp_rotate_dims()
+        dm.B, dm.L, dm.H, dm.Hk, dm.d = B, L, H, 0 if K is None else K.shape[1], d
+        for name, x, y in (("q", Q, out[0]), ("k", K, out[1])):
+            if x is not None:
+                self._mine(("out", y))
+                if y.shape != x.shape or y.dtype != x.dtype:
+                    raise ValueError("out: expected the shapes and type of Q and K")
+                _strides(y)
+                _check_written("out", y)
+                setattr(dm, name + "_stride", _free_strides(x))
+                setattr(dm, name + "o_stride", _free_strides(y))
+        _check(self.lib.fsharp_rotate(self._h, Q.data_ptr(), None if K is None else K.data_ptr(),
+                                      None if pos is None else pos.data_ptr(), pos.stride(0) if pos is not None and pos.dim() == 2 else 0,
+                                      pos0, C.byref(rope), C.byref(dm), _dtype_code(Q), int(bool(transpose)), out[0].data_ptr(),
+                                      None if K is None else out[1].data_ptr()), "fsharp_rotate")
+        return out
+
+    def _cross(self, Q, K, V, scale, key_len, key_mask):
+        """(dims, scale, key_len pointer, key_mask) of a cross attention, its tensors checked."""
+        B, H, Lq, d = Q.shape
+        if K.dim() != 4 or V.dim() != 4 or K.shape[0] != B or K.shape[3] != d or V.shape[:3] != K.shape[:3] \
+                or K.dtype != Q.dtype or V.dtype != Q.dtype:
+            raise ValueError(f"Q {tuple(Q.shape)} {Q.dtype}, K {tuple(K.shape)} {K.dtype}, V {tuple(V.shape)} {V.dtype}: expected "
+                             "[B,H,Lq,d], [B,Hk,Lk,d], [B,Hk,Lk,dv] of one type")
+        Hk, Lk = K.shape[1], K.shape[2]
+        if key_len is not None and (key_len.dtype != torch.int32 or tuple(key_len.shape) != (B,) or not key_len.is_contiguous()):
+            raise ValueError("key_len: expected a contiguous int32 [B] tensor")
+        if key_mask is not None:
+            if key_mask.dtype not in (torch.bool, torch.uint8) or tuple(key_mask.shape) not in ((B, Lk), (Lk,)) \
+                    or (Lk > 1 and key_mask.stride(-1) != 1):
+                raise ValueError("key_mask: expected bool or uint8 [B, Lk] or [Lk] whose last dimension is contiguous")
+        dm = fsharp_cross_dims()
+        dm.B, dm.H, dm.Hk, dm.Lq, dm.Lk, dm.d, dm.dv = B, H, Hk, Lq, Lk, d, V.shape[3]
+        dm.q_stride, dm.k_stride, dm.v_stride = _free_strides(Q), _free_strides(K), _free_strides(V)
+        dm.mask_stride = key_mask.stride(0) if key_mask is not None and key_mask.dim() == 2 else 0
+        return (dm, d ** -0.5 if scale is None else scale, None if key_len is None else key_len.data_ptr(),
+                None if key_mask is None else key_mask.data_ptr())
+
+    def _cross_scratch(self, dm, dtype, backward, device):
+        """The call's scratch: a tensor of its own each time, so that the allocator orders its reuse on the stream and a
+        captured graph keeps it in its pool."""
+        n = self.lib.fsharp_cross_scratch_bytes(self._h, C.byref(dm), dtype, backward)
+        _check(min(n, 0), "fsharp_cross_scratch_bytes")
+        return (torch.empty(n, dtype=torch.uint8, device=device) if n else None), n
+
+    def fsharp_cross_attend(self, Q, K, V, scale=None, key_len=None, key_mask=None, want_lse=False, out=None):
+        """Exact softmax attention of Q [B,H,Lq,d] to K [B,Hk,Lk,d], V [B,Hk,Lk,dv]: Y, or (Y, lse [B,H,Lq] float32) with
+        want_lse.  scale: d^-1/2 if None.  key_len: int32 [B].  key_mask: bool or uint8 [B,Lk] or [Lk], true where a key
+        is seen."""
+        self._mine(("Q", Q), ("K", K), ("V", V), ("key_len", key_len), ("key_mask", key_mask), ("out", out))
+        Q, K, V = _readable(Q), _readable(K), _readable(V)
+        dt = _dtype_code(Q)
+        dm, scale, lens, mask = self._cross(Q, K, V, scale, key_len, key_mask)
+        B, H, Lq, dv = dm.B, dm.H, dm.Lq, dm.dv
+        if out is None:
+            out = torch.empty(B, H, Lq, dv, dtype=Q.dtype, device=Q.device)
+        else:
+            if tuple(out.shape) != (B, H, Lq, dv) or out.dtype != Q.dtype:
+                raise ValueError(f"out: expected {(B, H, Lq, dv)} of {Q.dtype}")
+            _strides(out)
+            _check_written("out", out)
+        dm.y_stride = _free_strides(out)
+        lse = torch.empty(B, H, Lq, dtype=torch.float32, device=Q.device) if want_lse else None
+        scratch, n = self._cross_scratch(dm, dt, 0, Q.device)
+        _check(self.lib.fsharp_cross_attend(self._h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), lens, mask, C.byref(dm), dt, scale,
+                                            out.data_ptr(), lse.data_ptr() if want_lse else None,
+                                            scratch.data_ptr() if n else None, n), "fsharp_cross_attend")
+        return (out, lse) if want_lse else out
+
+    def fsharp_cross_attend_backward(self, Q, K, V, Y, lse, dY, scale=None, key_len=None, key_mask=None):
+        """(dQ, dK, dV) for the cotangent dY of fsharp_cross_attend's Y, with the Y and lse of that call; each gradient is a
+        new tensor with its tensor's shape and, where those are strides of places of its own, strides."""
+        self._mine(("Q", Q), ("K", K), ("V", V), ("Y", Y), ("lse", lse), ("dY", dY), ("key_len", key_len), ("key_mask", key_mask))
+        Q, K, V, Y, dY = (_readable(t) for t in (Q, K, V, Y, dY))
+        dt = _dtype_code(Q)
+        dm, scale, lens, mask = self._cross(Q, K, V, scale, key_len, key_mask)
+        rows = (dm.B, dm.H, dm.Lq)
+        for name, t in (("Y", Y), ("dY", dY)):
+            if tuple(t.shape) != rows + (dm.dv,) or t.dtype != Q.dtype:
+                raise ValueError(f"{name}: expected {rows + (dm.dv,)} of {Q.dtype}")
+        if tuple(lse.shape) != rows or lse.dtype != torch.float32 or not lse.is_contiguous():
+            raise ValueError(f"lse: expected a contiguous float32 tensor of shape {rows}")
+        dQ, dK, dV = (torch.empty_like(t) for t in (Q, K, V))      # (the strides of dense and permuted tensors, else dense)
+        dm.y_stride, dm.dy_stride = _free_strides(Y), _free_strides(dY)
+        dm.dq_stride, dm.dk_stride, dm.dv_stride = _free_strides(dQ), _free_strides(dK), _free_strides(dV)
+        scratch, n = self._cross_scratch(dm, dt, 1, Q.device)
+        _check(self.lib.fsharp_cross_attend_backward(
+            self._h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), Y.data_ptr(), lse.data_ptr(), dY.data_ptr(), lens, mask, C.byref(dm),
+            dt, scale, dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), scratch.data_ptr() if n else None, n),
+            "fsharp_cross_attend_backward")
+        return dQ, dK, dV
 
     def fsharp_forward_host(self, Q, K, V, Omega, variant, causal=False, chunk=0, pool=POOL_PER_BH,
                             qk_scale=1.0, out=None):

@@ -51,10 +51,12 @@ enum {
   FS_K_STATS = 1, FS_K_FIT, FS_K_PREP, FS_K_ROWTERM, FS_K_FEAT, FS_K_GROUPMAX, FS_K_KV,
   FS_K_PREFIX, FS_K_SCORES, FS_K_OUT, FS_K_PAIRS, FS_K_PAIRVAR_PREP, FS_K_PAIRVAR,
   FS_K_TC_KV, FS_K_TC_OUT, FS_K_TC_CAUSAL, FS_K_TC_STATS, FS_K_TC_ROWTERM, FS_K_TC_FEAT, FS_K_TC_KV128, FS_K_TC_OUT128,
-  FS_K_PAIR_IMAGES, FS_K_W3, FS_K_BWD_STATE, FS_K_BWD_NUMDEN, FS_K_BWD_DFEAT, FS_K_BWD_DX, FS_K_BWD_DV, FS_K_TC_MERGE,
+  FS_K_PAIR_IMAGES, FS_K_W3, FS_K_BWD_STATE, FS_K_BWD_NUMDEN, FS_K_BWD_DFEAT, FS_K_BWD_DX, FS_K_BWD_DV, FS_K_TC_MERGE, FS_K_ROTATE,
+  FS_K_CROSS_ROWS, FS_K_CROSS_FMA, FS_K_CROSS_JOIN, FS_K_CROSS_DELTA, FS_K_CROSS_DKV, FS_K_CROSS_DQ, FS_K_CROSS_SUM,
+  FS_K_TC_CROSS, FS_K_TC_CROSS_DKV, FS_K_TC_CROSS_DQ,
   FS_K_COUNT
 };
-static_assert(FS_K_COUNT <= 32, "ids are below 32");
+static_assert(FS_K_COUNT <= 64, "ids are below 64");
 constexpr int FS_TIMING_SLOTS = 4096;
 
 struct fsharp_ctx {
@@ -75,6 +77,19 @@ struct fsharp_ctx {
   // batch element); created on first use
   cudaStream_t copy_stream, down_stream;
   cudaEvent_t ev_inputs, ev_v;
+};
+
+// Makes `device` current for a call and puts the caller's back behind it.
+struct FsDevice {
+  int before = -1;
+  bool ok;
+  explicit FsDevice(int device) {
+    ok = cudaGetDevice(&before) == cudaSuccess && (before == device || cudaSetDevice(device) == cudaSuccess);
+    if (before == device) before = -1;
+  }
+  ~FsDevice() { if (before >= 0) cudaSetDevice(before); }
+  FsDevice(const FsDevice&) = delete;
+  FsDevice& operator=(const FsDevice&) = delete;
 };
 
 // NVTX range of a host-side stage (a no-op unless a tool that listens to NVTX is attached)

@@ -1,0 +1,55 @@
+// Exact cross attention: what its kernels share.  A unit is one (batch, key head); the R = (H / Hk) Lq query rows of the heads
+// that share the key head are its rows, row r = token r % Lq of the group's head r / Lq.  Scores live in the base-2 domain:
+// x = S log2(e), m a running maximum of x, l the sum of 2^(x - m).
+#pragma once
+
+#include "common.cuh"
+
+struct CrossArgs {
+  const void *Q, *K, *V;
+  TensorAddr aq, ak, av;
+  const int32_t* key_len;
+  const uint8_t* key_mask;
+  int64_t mask_stride;
+  int B, H, Hk, g, Lq, Lk, d, dv;
+  float scale;             // of the scores; kernels multiply by log2(e) where they need it
+};
+
+// The keys of sequence b: no more than this many.
+__device__ __forceinline__ int cross_keys(const CrossArgs& a, int b) {
+  return a.key_len ? max(0, min(a.Lk, a.key_len[b])) : a.Lk;
+}
+__device__ __forceinline__ bool cross_seen(const CrossArgs& a, int b, int j, int n) {
+  return j < n && (!a.key_mask || a.key_mask[b * a.mask_stride + j] != 0);
+}
+
+// Pieces of a unit's keys (or rows) that blocks of their own take, so that few units fill the GPU: partial results go to scratch.
+// Forward: O [unit][piece][R][dv] (unnormalised) and (m, l) [unit][piece][R].
+struct CrossPart {
+  float* o;
+  float2* ml;
+  int pieces;
+};
+
+#define FS_LN2 0.6931471805599453f
+
+// few rows (cross_rows.cu), and the join of pieces
+int fs_cross_rows_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype);
+int fs_cross_rows(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, TensorAddr ay, float* lse, CrossPart part);
+int fs_cross_join(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, TensorAddr ay, float* lse, CrossPart part);
+// multiply-add tiles (cross_fma.cu)
+int fs_cross_fma_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm);
+int fs_cross_fma(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, TensorAddr ay, float* lse, CrossPart part);
+
+// Backward.  stat [B][H][Lq]: (lse log2(e), D); partial sums of a piece: dK | dV [piece][unit][Lk][d + dv], dQ [piece][unit][R][d].
+struct CrossGrad {
+  const void* dY;
+  TensorAddr ady;
+  const float2* stat;
+  void *dQ, *dK, *dV;
+  TensorAddr adq, adk, adv;
+  float *pkv, *pq;             // null where the one piece writes the gradients themselves
+  int kv_pieces, q_pieces;
+};
+void fs_cross_fma_grad_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int* kv_pieces, int* q_pieces);
+int fs_cross_fma_grad(fsharp_ctx* ctx, const CrossArgs& a, int dtype, const CrossGrad& gr);

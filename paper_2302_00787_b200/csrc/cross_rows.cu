@@ -1,0 +1,255 @@
+// Cross attention of few query rows per key head (decoding steps): K and V are streamed once, straight from memory into
+// registers.  A key's d values lie across D / VE lanes (16 bytes each), a warp's load covers 512 bytes of K or V, and the
+// loads of four keys per lane and of their values are in flight together; scores are sums over a key's lanes by shuffles.
+// Each lane group keeps a maximum, a sum and an output of its own; they meet once at the end (warp, block, then the
+// pieces by cross_join_kernel).
+// Bound: HBM (2 n d bytes per element size and unit).
+#include "cross.cuh"
+#include "tc_common.cuh"
+
+namespace {
+
+constexpr int RW_T = 256, RW_WARPS = RW_T / 32, RW_U = 4;
+
+template <typename T> __device__ __forceinline__ void widen(const uint4& x, float* v);
+template <> __device__ __forceinline__ void widen<float>(const uint4& x, float* v) {
+  v[0] = __uint_as_float(x.x); v[1] = __uint_as_float(x.y); v[2] = __uint_as_float(x.z); v[3] = __uint_as_float(x.w);
+}
+template <> __device__ __forceinline__ void widen<__nv_bfloat16>(const uint4& x, float* v) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 4; i++) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+}
+
+__host__ __device__ constexpr int rows_step(int D, int es) { return RW_WARPS * (32 / (D * es / 16)) * RW_U; }    // keys per turn of a block
+
+template <typename T, int D, int R>
+__global__ void __launch_bounds__(RW_T)
+cross_rows_kernel(const __grid_constant__ CrossArgs a, T* __restrict__ Y, TensorAddr ay, float* __restrict__ lse, CrossPart part) {
+  constexpr int VE = 16 / (int)sizeof(T), LPK = D / VE, KPW = 32 / LPK, STEP = RW_WARPS * KPW * RW_U;
+  static_assert(STEP == rows_step(D, sizeof(T)), "");
+  __shared__ float so[RW_WARPS][R][D];
+  __shared__ float sm[RW_WARPS][R], sl[RW_WARPS][R];
+  const int unit = blockIdx.y, piece = blockIdx.x, b = unit / a.Hk, hk = unit % a.Hk, rows = a.g * a.Lq;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane / LPK, e0 = lane % LPK * VE;
+  const float c = a.scale * FS_LOG2E;
+  const bool inq = e0 < a.d, inv = e0 < a.dv;
+  float q[R][VE];
+#pragma unroll
+  for (int r = 0; r < R; r++) {
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (r < rows && inq)
+      x = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.Q) + b * a.aq.sb + (int64_t)(hk * a.g + r / a.Lq) * a.aq.sh +
+                                          (int64_t)(r % a.Lq) * a.aq.sl + e0);
+    widen<T>(x, q[r]);
+#pragma unroll
+    for (int k = 0; k < VE; k++) q[r][k] *= c;
+  }
+  const T* Kb = static_cast<const T*>(a.K) + b * a.ak.sb + hk * a.ak.sh + e0;
+  const T* Vb = static_cast<const T*>(a.V) + b * a.av.sb + hk * a.av.sh + e0;
+  const int n = cross_keys(a, b), turns = (n + STEP - 1) / STEP;
+  const int t0 = (int)((int64_t)turns * piece / part.pieces), t1 = (int)((int64_t)turns * (piece + 1) / part.pieces);
+  float m[R], l[R], o[R][VE];
+#pragma unroll
+  for (int r = 0; r < R; r++) {
+    m[r] = -INFINITY; l[r] = 0.f;
+#pragma unroll
+    for (int k = 0; k < VE; k++) o[r][k] = 0.f;
+  }
+  for (int t = t0; t < t1; t++) {
+    uint4 kx[RW_U], vx[RW_U];
+    bool seen[RW_U];
+#pragma unroll
+    for (int u = 0; u < RW_U; u++) {
+      const int j = t * STEP + (u * RW_WARPS + warp) * KPW + grp;
+      kx[u] = vx[u] = make_uint4(0, 0, 0, 0);
+      if (j < n && inq) kx[u] = __ldg(reinterpret_cast<const uint4*>(Kb + j * a.ak.sl));
+      if (j < n && inv) vx[u] = __ldg(reinterpret_cast<const uint4*>(Vb + j * a.av.sl));
+      seen[u] = cross_seen(a, b, j, n);
+    }
+    float s[RW_U][R];
+#pragma unroll
+    for (int u = 0; u < RW_U; u++) {
+      float k[VE];
+      widen<T>(kx[u], k);
+#pragma unroll
+      for (int r = 0; r < R; r++) {
+        float x = 0.f;
+#pragma unroll
+        for (int e = 0; e < VE; e++) x = fmaf(q[r][e], k[e], x);
+        s[u][r] = x;
+      }
+    }
+#pragma unroll
+    for (int w = 1; w < LPK; w <<= 1)
+#pragma unroll
+      for (int u = 0; u < RW_U; u++)
+#pragma unroll
+        for (int r = 0; r < R; r++) s[u][r] += __shfl_xor_sync(0xffffffffu, s[u][r], w);
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+      float top = m[r];
+#pragma unroll
+      for (int u = 0; u < RW_U; u++) {
+        if (!seen[u]) s[u][r] = -INFINITY;
+        top = fmaxf(top, s[u][r]);
+      }
+      const float base = top == -INFINITY ? 0.f : top, corr = tc::ex2(m[r] - base);
+      m[r] = top;
+      l[r] *= corr;
+#pragma unroll
+      for (int u = 0; u < RW_U; u++) {
+        s[u][r] = tc::ex2(s[u][r] - base);
+        l[r] += s[u][r];
+      }
+#pragma unroll
+      for (int e = 0; e < VE; e++) o[r][e] *= corr;
+    }
+#pragma unroll
+    for (int u = 0; u < RW_U; u++) {
+      if (!seen[u]) vx[u] = make_uint4(0, 0, 0, 0);      // what a hidden key holds may be anything
+      float v[VE];
+      widen<T>(vx[u], v);
+#pragma unroll
+      for (int r = 0; r < R; r++)
+#pragma unroll
+        for (int e = 0; e < VE; e++) o[r][e] = fmaf(s[u][r], v[e], o[r][e]);
+    }
+  }
+  // the warp's lane groups, then the block's warps
+#pragma unroll
+  for (int r = 0; r < R; r++) {
+    float top = m[r];
+#pragma unroll
+    for (int w = LPK; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+    const float f = tc::ex2(m[r] - (top == -INFINITY ? 0.f : top));
+    l[r] *= f;
+#pragma unroll
+    for (int e = 0; e < VE; e++) o[r][e] *= f;
+#pragma unroll
+    for (int w = LPK; w < 32; w <<= 1) {
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], w);
+#pragma unroll
+      for (int e = 0; e < VE; e++) o[r][e] += __shfl_xor_sync(0xffffffffu, o[r][e], w);
+    }
+    if (grp == 0) {
+#pragma unroll
+      for (int e = 0; e < VE; e++) so[warp][r][e0 + e] = o[r][e];
+      if (lane == 0) { sm[warp][r] = top; sl[warp][r] = l[r]; }
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < R * D; i += RW_T) {
+    const int r = i / D, e = i % D;
+    if (r >= rows || e >= a.dv) continue;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < RW_WARPS; w++) top = fmaxf(top, sm[w][r]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, x = 0.f;
+#pragma unroll
+    for (int w = 0; w < RW_WARPS; w++) {
+      const float f = tc::ex2(sm[w][r] - base);
+      sum = fmaf(f, sl[w][r], sum);
+      x = fmaf(f, so[w][r][e], x);
+    }
+    if (part.pieces > 1) {
+      const int64_t at = ((int64_t)unit * part.pieces + piece) * rows + r;
+      part.o[at * a.dv + e] = x;
+      if (e == 0) part.ml[at] = make_float2(top, sum);
+    } else {
+      const int h = hk * a.g + r / a.Lq, tok = r % a.Lq;
+      fs_store(Y + b * ay.sb + h * ay.sh + tok * ay.sl + e, sum == 0.f ? 0.f : x / sum);
+      if (lse && e == 0) lse[((int64_t)b * a.H + h) * a.Lq + tok] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * FS_LN2;
+    }
+  }
+}
+
+// Y and lse from the pieces' partial results: a thread per row and four values.
+template <typename T>
+__global__ void __launch_bounds__(256)
+cross_join_kernel(CrossPart part, int64_t units, int Hk, int R, int g, int Lq, int dv, T* __restrict__ Y, TensorAddr ay, float* __restrict__ lse) {
+  fs_grid_dependency_wait();
+  const int q = dv / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / q;
+  const int e = (int)(i % q) * 4;
+  if (row >= units * R) return;
+  const int64_t unit = row / R;
+  const int r = (int)(row % R);
+  float top = -INFINITY;
+  for (int p = 0; p < part.pieces; p++) top = fmaxf(top, part.ml[(unit * part.pieces + p) * R + r].x);
+  const float base = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int p = 0; p < part.pieces; p++) {
+    const int64_t at = (unit * part.pieces + p) * R + r;
+    const float2 ml = part.ml[at];
+    const float4 o = *reinterpret_cast<const float4*>(part.o + at * dv + e);
+    const float f = tc::ex2(ml.x - base);
+    sum = fmaf(f, ml.y, sum);
+    x.x = fmaf(f, o.x, x.x); x.y = fmaf(f, o.y, x.y); x.z = fmaf(f, o.z, x.z); x.w = fmaf(f, o.w, x.w);
+  }
+  const int64_t b = unit / Hk;
+  const int h = (int)(unit % Hk) * g + r / Lq, tok = r % Lq;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  T* y = Y + b * ay.sb + h * ay.sh + tok * ay.sl + e;
+  fs_store(y, x.x * inv); fs_store(y + 1, x.y * inv); fs_store(y + 2, x.z * inv); fs_store(y + 3, x.w * inv);
+  if (lse && e == 0) lse[(b * Hk * g + h) * Lq + tok] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * FS_LN2;
+}
+
+template <typename T, int D>
+void launch_rows(fsharp_ctx* ctx, const CrossArgs& a, T* Y, TensorAddr ay, float* lse, CrossPart part) {
+  const dim3 grid((unsigned)part.pieces, (unsigned)(a.B * a.Hk));
+  const int R = a.g * a.Lq;
+  if (R == 1) cross_rows_kernel<T, D, 1><<<grid, RW_T, 0, ctx->stream>>>(a, Y, ay, lse, part);
+  else if (R == 2) cross_rows_kernel<T, D, 2><<<grid, RW_T, 0, ctx->stream>>>(a, Y, ay, lse, part);
+  else cross_rows_kernel<T, D, 4><<<grid, RW_T, 0, ctx->stream>>>(a, Y, ay, lse, part);
+}
+
+template <typename T>
+int run_rows(fsharp_ctx* ctx, const CrossArgs& a, T* Y, TensorAddr ay, float* lse, CrossPart part) {
+  const int D = a.d > a.dv ? a.d : a.dv;
+  FS_TIME_BEGIN(ctx, FS_K_CROSS_ROWS);
+  if (D == 16) launch_rows<T, 16>(ctx, a, Y, ay, lse, part);
+  else if (D == 32) launch_rows<T, 32>(ctx, a, Y, ay, lse, part);
+  else if (D == 64) launch_rows<T, 64>(ctx, a, Y, ay, lse, part);
+  else launch_rows<T, 128>(ctx, a, Y, ay, lse, part);
+  FS_TIME_END(ctx);
+  FS_LAUNCH_CHECK(ctx);
+  return FSHARP_OK;
+}
+
+template <typename T>
+int run_join(fsharp_ctx* ctx, const CrossArgs& a, T* Y, TensorAddr ay, float* lse, CrossPart part) {
+  const int R = a.g * a.Lq;
+  const int64_t units = (int64_t)a.B * a.Hk, blocks = (units * R * (a.dv / 4) + 255) / 256;
+  if (blocks > 0x7fffffff) return FSHARP_E_SHAPE;
+  FS_TIME_BEGIN(ctx, FS_K_CROSS_JOIN);
+  FS_CUDA_OK(fs_launch_chained(cross_join_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, part, units, a.Hk, R, a.g, a.Lq,
+                               a.dv, Y, ay, lse));
+  FS_TIME_END(ctx);
+  FS_LAUNCH_CHECK(ctx);
+  return FSHARP_OK;
+}
+
+}  // namespace
+
+// As many pieces as fill the GPU with four blocks per SM, each with a turn of keys at least.
+int fs_cross_rows_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype) {
+  const int es = dtype == FSHARP_F32 ? 4 : 2, D = dm->d > dm->dv ? dm->d : dm->dv, step = rows_step(D, es);
+  const int64_t units = (int64_t)dm->B * dm->Hk, turns = ((int64_t)dm->Lk + step - 1) / step;
+  int64_t p = 4 * (int64_t)ctx->sm_count / units;
+  if (p > turns) p = turns;
+  if (p > 128) p = 128;
+  return p < 1 ? 1 : (int)p;
+}
+
+int fs_cross_rows(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, TensorAddr ay, float* lse, CrossPart part) {
+  return dtype == FSHARP_F32 ? run_rows<float>(ctx, a, static_cast<float*>(Y), ay, lse, part)
+                             : run_rows<__nv_bfloat16>(ctx, a, static_cast<__nv_bfloat16*>(Y), ay, lse, part);
+}
+int fs_cross_join(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, TensorAddr ay, float* lse, CrossPart part) {
+  return dtype == FSHARP_F32 ? run_join<float>(ctx, a, static_cast<float*>(Y), ay, lse, part)
+                             : run_join<__nv_bfloat16>(ctx, a, static_cast<__nv_bfloat16*>(Y), ay, lse, part);
+}

@@ -176,6 +176,17 @@ const char* fsharp_kernel_name(int id) {
     case FS_K_TC_FEAT: return "tc_feat_kernel";
     case FS_K_TC_KV128: return "tc_kv128_kernel";
     case FS_K_TC_OUT128: return "tc_out128_kernel";
+    case FS_K_ROTATE: return "rotate_kernel";
+    case FS_K_CROSS_ROWS: return "cross_rows_kernel";
+    case FS_K_CROSS_FMA: return "cross_fma_kernel";
+    case FS_K_CROSS_JOIN: return "cross_join_kernel";
+    case FS_K_CROSS_DELTA: return "cross_delta_kernel";
+    case FS_K_CROSS_DKV: return "cross_dkv_kernel";
+    case FS_K_CROSS_DQ: return "cross_dq_kernel";
+    case FS_K_CROSS_SUM: return "cross_sum_kernel";
+    case FS_K_TC_CROSS: return "tc_cross_kernel";
+    case FS_K_TC_CROSS_DKV: return "tc_cross_dkv_kernel";
+    case FS_K_TC_CROSS_DQ: return "tc_cross_dq_kernel";
     default: return "";
   }
 }
