@@ -159,13 +159,13 @@ def _strides(t: torch.Tensor):
 
 def _readable(t: torch.Tensor) -> torch.Tensor:
     """`t`, or a dense copy where its strides cannot be told to the library: a tensor broadcast along every dimension
-    (three zeros mean dense there), rows or a start that are not 16-byte aligned, a last dimension with gaps."""
+    (three zeros mean dense there) or along its tokens, rows or a start that are not 16-byte aligned, a last dimension with gaps."""
     if t.dim() != 4:
         raise ValueError("expected a [B, H, L, inner] tensor")
     es = t.element_size()
     strides = [s for s, n in zip(t.stride()[:3], t.shape[:3]) if n > 1]
     if (t.shape[3] > 1 and t.stride(3) != 1) or (strides and not any(strides)) or any(s * es % 16 for s in strides) \
-            or t.data_ptr() % 16:
+            or (t.shape[2] > 1 and t.stride(2) == 0) or t.data_ptr() % 16:
         return t.contiguous() if not t.is_contiguous() else t.clone()
     return t
 

@@ -101,7 +101,13 @@ int check_tensor(const void* p, int dtype, const int64_t s[3]) {
   return FSHARP_OK;
 }
 
-enum Kind { ROWS, FMA };
+// K or V: the same, and a token stride that tells the keys apart.
+int check_keys(const void* p, int dtype, const int64_t s[3], int Lk) {
+  FS_TRY(check_tensor(p, dtype, s));
+  return Lk > 1 && s[2] == 0 && (s[0] != 0 || s[1] != 0) ? FSHARP_E_SHAPE : FSHARP_OK;
+}
+
+enum Kind { ROWS, FMA, TC };
 struct Plan {
   Kind kind;
   int pieces;
@@ -111,8 +117,11 @@ struct Plan {
 Plan plan_forward(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype) {
   Plan p = {};
   const int64_t R = (int64_t)dm->H / dm->Hk * dm->Lq, units = (int64_t)dm->B * dm->Hk;
-  p.kind = R < FSHARP_CROSS_FEW_ROWS && ctx->impl != FSHARP_IMPL_TENSOR ? ROWS : FMA;
-  p.pieces = p.kind == ROWS ? fs_cross_rows_pieces(ctx, dm, dtype) : fs_cross_fma_pieces(ctx, dm);
+  if (ctx->impl == FSHARP_IMPL_TENSOR) p.kind = TC;
+  else if (R < FSHARP_CROSS_FEW_ROWS) p.kind = ROWS;
+  else p.kind = dtype == FSHARP_BF16 && ctx->impl == FSHARP_IMPL_AUTO ? TC : FMA;
+  if (dm->Lk == 0) p.kind = FMA;       // (zeros: there is no key that a tensor map could describe)
+  p.pieces = p.kind == ROWS ? fs_cross_rows_pieces(ctx, dm, dtype) : p.kind == TC ? fs_tc_cross_pieces(ctx, dm) : fs_cross_fma_pieces(ctx, dm);
   if (p.pieces > 1) {
     p.ml = units * p.pieces * R;
     p.o_floats = p.ml * dm->dv;
@@ -177,8 +186,8 @@ int fsharp_cross_attend(fsharp_ctx* ctx, const void* Q, const void* K, const voi
   if ((int64_t)dims->B * dims->H == 0 || dims->Lq == 0) return FSHARP_OK;
   FS_TRY(check_tensor(Q, dtype, dims->q_stride));
   if (dims->Lk) {                     // (without keys K and V are not read)
-    FS_TRY(check_tensor(K, dtype, dims->k_stride));
-    FS_TRY(check_tensor(V, dtype, dims->v_stride));
+    FS_TRY(check_keys(K, dtype, dims->k_stride, dims->Lk));
+    FS_TRY(check_keys(V, dtype, dims->v_stride, dims->Lk));
   }
   FS_TRY(check_tensor(Y, dtype, dims->y_stride));
   const Plan p = plan_forward(ctx, dims, dtype);
@@ -194,6 +203,7 @@ int fsharp_cross_attend(fsharp_ctx* ctx, const void* Q, const void* K, const voi
     part.ml = ws.take<float2>(p.ml);
   }
   if (p.kind == ROWS) FS_TRY(fs_cross_rows(ctx, a, dtype, Y, ay, lse, part));
+  else if (p.kind == TC) FS_TRY(fs_tc_cross(ctx, a, Y, ay, lse, part));
   else FS_TRY(fs_cross_fma(ctx, a, dtype, Y, ay, lse, part));
   return p.pieces > 1 ? fs_cross_join(ctx, a, dtype, Y, ay, lse, part) : FSHARP_OK;
 }
@@ -213,8 +223,8 @@ int fsharp_cross_attend_backward(fsharp_ctx* ctx, const void* Q, const void* K, 
   FS_TRY(check_tensor(dQ, dtype, dims->dq_stride));
   if (!lse) return FSHARP_E_BADARG;
   if (dims->Lk) {
-    FS_TRY(check_tensor(K, dtype, dims->k_stride));
-    FS_TRY(check_tensor(V, dtype, dims->v_stride));
+    FS_TRY(check_keys(K, dtype, dims->k_stride, dims->Lk));
+    FS_TRY(check_keys(V, dtype, dims->v_stride, dims->Lk));
     FS_TRY(check_tensor(dK, dtype, dims->dk_stride));
     FS_TRY(check_tensor(dV, dtype, dims->dv_stride));
   }

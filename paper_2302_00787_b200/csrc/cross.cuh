@@ -33,6 +33,10 @@ struct CrossPart {
 
 #define FS_LN2 0.6931471805599453f
 
+// tensor cores (tc_cross.cu): bf16
+int fs_tc_cross_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm);
+int fs_tc_cross(fsharp_ctx* ctx, const CrossArgs& a, void* Y, TensorAddr ay, float* lse, CrossPart part);
+
 // few rows (cross_rows.cu), and the join of pieces
 int fs_cross_rows_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype);
 int fs_cross_rows(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, TensorAddr ay, float* lse, CrossPart part);

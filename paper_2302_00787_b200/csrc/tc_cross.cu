@@ -1,0 +1,386 @@
+// Exact cross attention of bf16 tensors on the tensor cores:  Y = softmax(scale Q K^T) V  with a running maximum.
+//
+// A block has up to 256 rows of a unit (rows are packed over the query heads that share a key head) and walks the unit's keys
+// in tiles of 128.  Two warpgroups, thread = row: each has scores S (128 lanes x 128 columns of tensor memory), from which its
+// threads read a row, take the maximum and the exponentials and put them back as bf16 P over S, and an output O that the
+// tensor core adds P V to from there.  Warps of their own copy K and V tiles (TMA, one ring, K before V) and issue the
+// products: S of the next tile and P V of one warpgroup run while the other one is at its exponentials.
+// With more than 128 rows the warpgroups take 128 rows each and share every K and V tile; with fewer they take the tiles in
+// turn, as if one were another piece of the keys, and meet in shared memory at the end.
+// O is only rescaled when a row's maximum has grown by more than 2^8 (every factor is exact in the sense that l and O have the
+// same one); P is then at most 2^8, which bf16 holds as well as 1.
+// P is rounded to bf16 (2^-8 relative) as the tensor core's operand; l sums the exponentials before that rounding, in fp32.
+// Bound: exponentials (128 x 128 per tile and warpgroup; part of them by a cubic on the multiply-add pipe) and issue slots.
+#include "cross.cuh"
+#include "tc_common.cuh"
+#include "tc_layout.cuh"
+
+using namespace tc;
+using namespace tcl;
+
+namespace {
+
+constexpr int CX_WARPS = 8, CXW_TMA = 8, CXW_MMA = 9, CX_T = 384;      // (warps 10, 11 only hand their registers over)
+constexpr uint32_t CX_TMEM = 512, CX_S = 0, CX_O = 256;      // S of the two warpgroups, then O (128 columns apart)
+constexpr float CX_SLACK = 8.f;
+
+template <int D>
+struct CxSm {
+  static constexpr int PANELS = D / 64, NS = D == 64 ? 8 : 5;      // slots of the ring: a K or V tile each
+  static constexpr uint32_t SLOT = PANELS * TILE_BYTES, Q = 0, RING = 2 * SLOT, MISC = RING + NS * SLOT, TOTAL = MISC + 512;
+  static_assert(TOTAL + 1024 <= 232448, "shared memory budget");
+  static_assert(NS * SLOT >= 128 * (D + 1) * 4 + 1024, "the warpgroups' exchange");
+};
+struct CxMs {
+  uint64_t full[8], empty[8], s_full[2], p_ready[2], o_full[2], q_ready;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+static_assert(sizeof(CxMs) <= 512, "misc block");
+
+// max of three that hands NaNs on
+__device__ __forceinline__ float max3n(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ void fma2(uint32_t& a, uint32_t& b, float m, float n) {      // (a, b) = (a, b) m + n
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
+      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "+r"(a), "+r"(b)
+      : "f"(m), "f"(n));
+}
+
+template <int D>
+__global__ void __launch_bounds__(CX_T, 1)
+tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CrossArgs a,
+                __nv_bfloat16* __restrict__ Y, TensorAddr ay, float* __restrict__ lse, CrossPart part, int* __restrict__ status) {
+  using Sm = CxSm<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  CxMs* misc = reinterpret_cast<CxMs*>(sm + Sm::MISC);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* abortp = &misc->abort_flag;
+  const int unit = blockIdx.y, piece = blockIdx.x % part.pieces, r0 = (int)(blockIdx.x / part.pieces) * 256;
+  const int b = unit / a.Hk, hk = unit % a.Hk, R = a.g * a.Lq;
+  const int n = cross_keys(a, b), tiles = (n + TILE - 1) / TILE;
+  const int t0 = (int)((int64_t)tiles * piece / part.pieces), nt = (int)((int64_t)tiles * (piece + 1) / part.pieces) - t0;
+  const bool both = R - r0 > TILE;                     // each warpgroup has rows of its own
+  const int items = both ? 2 * nt : nt;                // item i: warpgroup i & 1, tile i / 2 or i
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < Sm::NS; i++) { mbar_init(&misc->full[i], 1); mbar_init(&misc->empty[i], 1); }
+    for (int w = 0; w < 2; w++) { mbar_init(&misc->s_full[w], 1); mbar_init(&misc->p_ready[w], 4); mbar_init(&misc->o_full[w], 1); }
+    mbar_init(&misc->q_ready, CX_WARPS);
+    misc->abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == CXW_MMA) {
+    tmem_alloc(&misc->tmem_base, CX_TMEM);
+    tmem_relinquish();
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  tcgen05_fence_after();
+  const uint32_t tmem = misc->tmem_base;
+  const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;      // panels of 64 columns
+
+  if (warp >= CX_WARPS) regs_release<REGS_PRODUCER>();
+  if (warp == CXW_TMA) {
+    if (lane == 0) {
+      prefetch_tmap(&tmK); prefetch_tmap(&tmV);
+      bool ok = true;
+      int issued = 0;
+      // (a stride of zero, one entry for all, is a dimension of size one in the tensor map)
+      const int ch[2] = {a.ak.sh ? hk : 0, a.av.sh ? hk : 0}, cb[2] = {a.ak.sb ? b : 0, a.av.sb ? b : 0};
+      for (; issued < 2 * nt && ok; issued++) {
+        const int s = issued % Sm::NS, tok = (t0 + issued / 2) * TILE;
+        if (!mbar_wait(&misc->empty[s], ((issued / Sm::NS) & 1) ^ 1, abortp, status)) { ok = false; break; }
+        uint8_t* base = sm + Sm::RING + s * Sm::SLOT;
+        const CUtensorMap* map = issued & 1 ? &tmV : &tmK;
+        const int panels = issued & 1 ? vp : kp;
+        mbar_expect_tx(&misc->full[s], panels * TILE_BYTES);
+        for (int p = 0; p < panels; p++) tma_load_4d(base + p * TILE_BYTES, map, &misc->full[s], p * 64, tok, ch[issued & 1], cb[issued & 1]);
+      }
+      // no copy of this block may still be in flight when it exits
+      for (int i = max(0, issued - Sm::NS); i < issued; i++) mbar_wait(&misc->full[i % Sm::NS], (i / Sm::NS) & 1, abortp, status, false);
+    }
+  } else if (warp == CXW_MMA) {
+    // The whole warp walks the schedule (waits and descriptor arithmetic stay warp-uniform); an elected lane issues.
+    constexpr uint32_t ID_S = idesc_bf16(128, 128, 0, 0);
+    const uint32_t ID_O = idesc_bf16(128, a.dv, 0, 1);
+    const uint32_t sQ = smem_u32(sm + Sm::Q), sR = smem_u32(sm + Sm::RING);
+    const int ksteps = a.d / 16;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abortp, status)) != 0; };
+    auto issue_s = [&](int i) {                        // S of item i
+      const int w = i & 1, t = both ? i >> 1 : i, slot = 2 * t % Sm::NS;
+      if (!wait(&misc->full[slot], (2 * t / Sm::NS) & 1)) return false;
+      tcgen05_fence_after();
+      const uint64_t dQ = smem_desc(sQ + (both ? w : 0) * Sm::SLOT, 16, 1024, SWZ_128B), dK = smem_desc(sR + slot * Sm::SLOT, 16, 1024, SWZ_128B);
+      if (elect_one()) {
+        for (int k = 0; k < ksteps; k++) {
+          const uint32_t off = (k >> 2) * TILE_BYTES + (k & 3) * 32;
+          mma_bf16(tmem + CX_S + w * 128, desc_advance(dQ, off), desc_advance(dK, off), ID_S, k > 0);
+        }
+        if (!both || w) mma_commit(&misc->empty[slot]);
+        mma_commit(&misc->s_full[w]);
+      }
+      __syncwarp();
+      return true;
+    };
+    bool ok = nt > 0 && wait(&misc->q_ready, 0);
+    if (ok) {
+      tcgen05_fence_after();
+      ok = issue_s(0) && (items < 2 || issue_s(1));
+    }
+    for (int i = 0; i < items && ok; i++) {
+      const int w = i & 1, t = both ? i >> 1 : i, slot = (2 * t + 1) % Sm::NS;
+      ok = wait(&misc->full[slot], ((2 * t + 1) / Sm::NS) & 1) && wait(&misc->p_ready[w], (i >> 1) & 1);
+      if (!ok) break;
+      tcgen05_fence_after();
+      // V: panels of 64 columns (leading offset = their distance), 16 keys per step = 16 rows of 128 bytes
+      const uint64_t dV = smem_desc(sR + slot * Sm::SLOT, TILE_BYTES, 1024, SWZ_128B);
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < 8; k++)
+          mma_bf16_ta(tmem + CX_O + w * 128, tmem + CX_S + w * 128 + 8 * k, desc_advance(dV, k * 2048), ID_O, i > 1 || k > 0);
+        if (!both || w) mma_commit(&misc->empty[slot]);
+        if (i + 2 >= items) mma_commit(&misc->o_full[w]);
+      }
+      __syncwarp();
+      if (i + 2 < items) ok = issue_s(i + 2);
+    }
+  } else if (warp < CX_WARPS) {
+    regs_acquire<REGS_EPILOGUE>();
+    const int w = warp >> 2, row = (warp & 3) * 32 + lane;
+    {
+      // the block's rows of Q into shared memory, rows and columns that there are none of as zeros
+      constexpr int CH = D / 8;
+      const int rows = both ? 256 : 128;
+      const __nv_bfloat16* Q = static_cast<const __nv_bfloat16*>(a.Q) + b * a.aq.sb;
+      for (int i = threadIdx.x; i < rows * CH; i += 256) {
+        const int rr = i / CH, ch = i % CH, r = r0 + rr;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (r < R && ch * 8 < a.d) x = *reinterpret_cast<const uint4*>(Q + (int64_t)(hk * a.g + r / a.Lq) * a.aq.sh + (int64_t)(r % a.Lq) * a.aq.sl + ch * 8);
+        *reinterpret_cast<uint4*>(sm + Sm::Q + (rr >> 7) * Sm::SLOT + (ch >> 3) * TILE_BYTES + sw128_offset(rr & 127, (ch & 7) * 8)) = x;
+      }
+      fence_proxy_async_smem();
+      mbar_arrive_warp(&misc->q_ready, lane);
+    }
+    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), tS = lanes + CX_S + w * 128, tO = lanes + CX_O + w * 128;
+    const int first = r0 + (both ? w * TILE : 0), r = first + row;      // this thread's row
+    const bool idle = first + (warp & 3) * 32 >= R;                     // no row of this warp exists
+    const int mine = both ? nt : (nt + 1 - w) / 2;                      // its tiles
+    const float c = fmaxf(a.scale * FS_LOG2E, 1.2e-38f);                // (hidden scores are -inf: 0 would make them NaN)
+    float m = -INFINITY;
+    uint32_t l[2] = {0u, 0u};
+    bool ok = true;
+    for (int i = 0; i < mine; i++) {
+      const int t = both ? i : 2 * i + w, j0 = (t0 + t) * TILE;
+      uint32_t seen[4];
+      const bool some = a.key_mask != nullptr || j0 + TILE > n;         // some key of the tile may be hidden
+      if (some) {
+#pragma unroll
+        for (int q = 0; q < 4; q++) seen[q] = __ballot_sync(0xffffffffu, cross_seen(a, b, j0 + q * 32 + lane, n));
+        if (!both || w == 0) {
+          // what a hidden key's V holds may be anything: zeros in its place, thread = key (one warpgroup does it for both: the
+          // other's product is issued behind its own)
+          const int slot = (2 * t + 1) % Sm::NS;
+          ok = __all_sync(0xffffffffu, mbar_wait(&misc->full[slot], ((2 * t + 1) / Sm::NS) & 1, abortp, status, false));
+          if (ok && !(seen[warp & 3] >> lane & 1u))
+            for (int p = 0; p < vp; p++)
+              for (int k = 0; k < 8; k++)
+                *reinterpret_cast<uint4*>(sm + Sm::RING + slot * Sm::SLOT + p * TILE_BYTES + row * 128 + k * 16) = make_uint4(0, 0, 0, 0);
+          fence_proxy_async_smem();
+        }
+      }
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(&misc->s_full[w], i & 1, abortp, status, false));
+      if (!ok) break;
+      tcgen05_fence_after();
+      if (!idle) {
+        uint32_t s[128];
+#pragma unroll
+        for (int q = 0; q < 8; q++) tmem_ld16(tS + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(s + 16 * q));
+        tmem_wait_ld();
+        if (some) {
+#pragma unroll
+          for (int q = 0; q < 128; q++) s[q] = (seen[q >> 5] >> (q & 31)) & 1u ? s[q] : 0xff800000u;
+        }
+        float top = __uint_as_float(s[0]);
+        {
+          float t1 = __uint_as_float(s[1]), t2 = __uint_as_float(s[2]), t3 = __uint_as_float(s[3]);
+#pragma unroll
+          for (int q = 4; q < 124; q += 8) {
+            top = max3n(top, __uint_as_float(s[q]), __uint_as_float(s[q + 1]));
+            t1 = max3n(t1, __uint_as_float(s[q + 2]), __uint_as_float(s[q + 3]));
+            t2 = max3n(t2, __uint_as_float(s[q + 4]), __uint_as_float(s[q + 5]));
+            t3 = max3n(t3, __uint_as_float(s[q + 6]), __uint_as_float(s[q + 7]));
+          }
+          top = max3n(top, __uint_as_float(s[124]), __uint_as_float(s[125]));
+          t1 = max3n(t1, __uint_as_float(s[126]), __uint_as_float(s[127]));
+          top = max3n(max3n(top, t1, t2), t3, t3);
+        }
+        top *= c;
+        // (an infinite score makes the row NaN as its definition does: the cubic below would drop inf - inf)
+        if (top == INFINITY) top = __uint_as_float(0x7fc00000u);
+        const bool grown = !(top <= m + CX_SLACK) && top != -INFINITY;
+        if (__any_sync(0xffffffffu, grown)) {
+          const float f = grown ? ex2(m - top) : 1.f;
+          if (grown) m = top;
+          l[0] = __float_as_uint(__uint_as_float(l[0]) * f);
+          l[1] = __float_as_uint(__uint_as_float(l[1]) * f);
+          if (i > 0) {
+            for (int q = 0; q < a.dv; q += 16) {
+              uint32_t o[16];
+              tmem_ld16(tO + q, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int k = 0; k < 16; k++) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+              tmem_st16(tO + q, o);
+            }
+          }
+        }
+        const float base = m == -INFINITY ? 0.f : -m;
+#pragma unroll
+        for (int q = 0; q < 128; q += 32) {
+          uint32_t o[16];
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) {
+            fma2(s[q + k], s[q + k + 1], c, base);
+            if ((k & 7) < 4) {
+              s[q + k] = __float_as_uint(ex2(__uint_as_float(s[q + k])));
+              s[q + k + 1] = __float_as_uint(ex2(__uint_as_float(s[q + k + 1])));
+            } else {
+              exp2_poly2(s[q + k], s[q + k + 1]);
+            }
+            add2(l[0], l[1], __uint_as_float(s[q + k]), __uint_as_float(s[q + k + 1]));
+            o[k / 2] = pack_bf16(__uint_as_float(s[q + k]), __uint_as_float(s[q + k + 1]));
+          }
+          tmem_st16(tS + q / 2, o);
+        }
+        tmem_wait_st();
+      }
+      tcgen05_fence_before();
+      mbar_arrive_warp(&misc->p_ready[w], lane);
+    }
+    // all products are done before anything of the ring is written below
+    if (ok && mine > 0) ok = mbar_wait(&misc->o_full[w], 0, abortp, status, false);
+    if (ok && !both && (nt + w) / 2 > 0) ok = mbar_wait(&misc->o_full[w ^ 1], 0, abortp, status, false);
+    ok = __all_sync(0xffffffffu, ok);
+    tcgen05_fence_after();
+    float sum = m == -INFINITY ? 0.f : __uint_as_float(l[0]) + __uint_as_float(l[1]);      // (2^-125 per hidden key from the cubic)
+    // (every warp comes to the barriers below, also after a wait that ran out)
+    float* xo = reinterpret_cast<float*>(sm + Sm::RING);                // [128][D + 1]
+    float2* xm = reinterpret_cast<float2*>(sm + Sm::RING + 128 * (D + 1) * 4);
+    if (!both) {
+      if (w == 1 && ok) {
+        for (int q = 0; q < a.dv; q += 16) {
+          uint32_t o[16] = {};
+          if (mine > 0) {
+            tmem_ld16(tO + q, o);
+            tmem_wait_ld();
+          }
+#pragma unroll
+          for (int k = 0; k < 16; k++) xo[row * (D + 1) + q + k] = __uint_as_float(o[k]);
+        }
+        xm[row] = make_float2(m, sum);
+      }
+      named_bar_sync(3, 256);
+    }
+    if ((both || w == 0) && ok) {
+      float f0 = 1.f, f1 = 0.f;
+      if (!both) {
+        const float2 other = xm[row];
+        const float top = fmaxf(m, other.x), base = top == -INFINITY ? 0.f : top;
+        f0 = ex2(m - base); f1 = ex2(other.x - base);
+        sum = sum * f0 + other.y * f1;
+        m = top;
+      }
+      const int h = hk * a.g + r / a.Lq, tok = r % a.Lq;
+      const float inv = part.pieces > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+      const int64_t at = ((int64_t)unit * part.pieces + piece) * R + r;
+      __nv_bfloat16* y = Y + b * ay.sb + h * ay.sh + tok * ay.sl;
+      for (int q = 0; q < a.dv; q += 16) {
+        uint32_t o[16] = {};
+        if (mine > 0) {
+          tmem_ld16(tO + q, o);
+          tmem_wait_ld();
+        }
+        float x[16];
+#pragma unroll
+        for (int k = 0; k < 16; k++) {
+          x[k] = __uint_as_float(o[k]);
+          // (a warpgroup that saw nothing has a factor of zero; its sums are zeros)
+          if (!both) x[k] = x[k] * f0 + xo[row * (D + 1) + q + k] * f1;
+          x[k] *= inv;
+        }
+        if (r < R) {
+          if (part.pieces > 1) {
+#pragma unroll
+            for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(part.o + at * a.dv + q + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 16; k += 8)
+              *reinterpret_cast<uint4*>(y + q + k) = make_uint4(pack_bf16(x[k], x[k + 1]), pack_bf16(x[k + 2], x[k + 3]), pack_bf16(x[k + 4], x[k + 5]), pack_bf16(x[k + 6], x[k + 7]));
+          }
+        }
+      }
+      if (r < R) {
+        if (part.pieces > 1) part.ml[at] = make_float2(m, sum);
+        else if (lse) lse[((int64_t)b * a.H + h) * a.Lq + tok] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * FS_LN2;
+      }
+    }
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  if (warp == CXW_MMA) {
+    tcgen05_fence_after();
+    tmem_dealloc(tmem, CX_TMEM);
+  }
+}
+
+template <int D>
+int launch(fsharp_ctx* ctx, const CUtensorMap& tmK, const CUtensorMap& tmV, const CrossArgs& a, void* Y, TensorAddr ay, float* lse, CrossPart part) {
+  const int64_t gx = ((int64_t)a.g * a.Lq + 255) / 256 * part.pieces;
+  if (gx > 0x7fffffff) return FSHARP_E_SHAPE;
+  FS_CUDA_OK(fs_allow_smem(tc_cross_kernel<D>));
+  FS_TIME_BEGIN(ctx, FS_K_TC_CROSS);
+  tc_cross_kernel<D><<<dim3((unsigned)gx, (unsigned)(a.B * a.Hk)), CX_T, CxSm<D>::TOTAL + 1024, ctx->stream>>>(
+      tmK, tmV, a, static_cast<__nv_bfloat16*>(Y), ay, lse, part, ctx->d_status);
+  FS_TIME_END(ctx);
+  FS_LAUNCH_CHECK(ctx);
+  return FSHARP_OK;
+}
+
+}  // namespace
+
+namespace tchost {
+int make_map_tokens(CUtensorMap* map, const void* base, TensorAddr a, int B, int H, int L, int inner);
+}
+
+// Keys or values as a tensor map.  A dimension of size one may carry any stride, which nothing reads; one whose entries are all the
+// same (stride zero) becomes a dimension of size one.
+int fs_tc_cross_map(CUtensorMap* map, const void* base, TensorAddr t, int B, int H, int L, int inner) {
+  if (t.sh == 0) H = 1;
+  if (t.sb == 0) B = 1;
+  if (L == 1) t.sl = inner;
+  if (H == 1) t.sh = t.sl * L;
+  if (B == 1) t.sb = t.sh * H;
+  return tchost::make_map_tokens(map, base, t, B, H, L, inner);
+}
+
+// Pieces that bring the blocks up to one per SM, each with two tiles at least.
+int fs_tc_cross_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm) {
+  const int64_t R = (int64_t)dm->H / dm->Hk * dm->Lq, blocks = (int64_t)dm->B * dm->Hk * ((R + 255) / 256), tiles = ((int64_t)dm->Lk + TILE - 1) / TILE;
+  int64_t p = ctx->sm_count / blocks;
+  if (p > tiles / 2) p = tiles / 2;
+  if (p > 64) p = 64;
+  return p < 1 ? 1 : (int)p;
+}
+
+int fs_tc_cross(fsharp_ctx* ctx, const CrossArgs& a, void* Y, TensorAddr ay, float* lse, CrossPart part) {
+  CUtensorMap tmK, tmV;
+  FS_TRY(fs_tc_cross_map(&tmK, a.K, a.ak, a.B, a.Hk, a.Lk, a.d));
+  FS_TRY(fs_tc_cross_map(&tmV, a.V, a.av, a.B, a.Hk, a.Lk, a.dv));
+  return a.d > 64 || a.dv > 64 ? launch<128>(ctx, tmK, tmV, a, Y, ay, lse, part) : launch<64>(ctx, tmK, tmV, a, Y, ay, lse, part);
+}

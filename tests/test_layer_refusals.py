@@ -86,6 +86,8 @@ def test_cross(lib, blank, backward):
         assert go(null=(n,)) == BADARG, n
         assert go(move=(n,)) == ALIGN, n
         assert go(**{n + "_stride": (6400, 3200, 33)}) == ALIGN, n
+    for n in ("k", "v"):
+        assert go(**{n + "_stride": (6400, 3200, 0)}) == SHAPE
     if backward:
         assert go(null=("lse",)) == BADARG
         assert go(scratch=None) == BADARG and go(scratch=P + 4) == ALIGN and go(nbytes=16) == NOMEM
