@@ -324,7 +324,7 @@ int fsharp_rotate(fsharp_ctx* ctx, const void* Q, const void* K, const int64_t* 
  * bf16 runs on the tensor cores (fewer than FSHARP_CROSS_FEW_ROWS query rows per key head: multiply-add kernels that
  * stream K and V), fp32 on the multiply-add pipe in fp32 throughout.  FSHARP_IMPL_SIMT forces the multiply-add kernels;
  * FSHARP_IMPL_TENSOR refuses fp32 (FSHARP_E_SHAPE).  B * Hk <= 65535.  Strides of zero (one entry for a whole dimension)
- * are allowed but for the tokens of K and V (FSHARP_E_SHAPE), and never in what is written. */
+ * are allowed, but not for the tokens of K, V and, backward, Q and dY (FSHARP_E_SHAPE), and never in what is written. */
 #define FSHARP_CROSS_FEW_ROWS 5
 typedef struct {
   int32_t B, H, Hk, Lq, Lk, d, dv;

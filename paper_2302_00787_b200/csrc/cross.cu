@@ -6,20 +6,20 @@
 
 namespace {
 
-// (lse log2(e), D = dY . Y) of every row; a row that sees nothing gets +inf, which makes its every 2^(x - lse) zero.  LPR lanes share
-// a row's dv values, 16 bytes each.
+// -lse log2(e) and -D, D = dY . Y, of every row and of the places up to a multiple of 64 (cross.cuh).  dv / VE lanes share a
+// row's dv values, 16 bytes each.
 template <typename T>
 __global__ void __launch_bounds__(256)
 cross_delta_kernel(const T* __restrict__ Y, TensorAddr ay, const T* __restrict__ dY, TensorAddr ady, const float* __restrict__ lse,
-                   int64_t rows, int H, int Lq, int dv, float2* __restrict__ stat) {
+                   int64_t places, int H, int Lq, int dv, float* __restrict__ stat) {
   constexpr int VE = 16 / (int)sizeof(T);
-  const int lpr = dv / VE;                           // 2 .. 32, a power of two
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / lpr;
-  const int e = (int)(i % lpr) * VE;
+  const int lpr = dv / VE, Lp = (Lq + 63) / 64 * 64;  // lpr: 2 .. 32, a power of two
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, place = i / lpr, bh = place / Lp;
+  const int e = (int)(i % lpr) * VE, tok = (int)(place % Lp);
+  const bool row = place < places && tok < Lq;
   float sum = 0.f;
-  if (row < rows) {
-    const int64_t b = row / ((int64_t)H * Lq);
-    const int h = (int)(row / Lq % H), tok = (int)(row % Lq);
+  if (row) {
+    const int64_t b = bh / H, h = bh % H;
     const uint4 y = *reinterpret_cast<const uint4*>(Y + b * ay.sb + h * ay.sh + tok * ay.sl + e);
     const uint4 g = *reinterpret_cast<const uint4*>(dY + b * ady.sb + h * ady.sh + tok * ady.sl + e);
     const T *py = reinterpret_cast<const T*>(&y), *pg = reinterpret_cast<const T*>(&g);
@@ -27,9 +27,11 @@ cross_delta_kernel(const T* __restrict__ Y, TensorAddr ay, const T* __restrict__
     for (int k = 0; k < VE; k++) sum = fmaf(fs_load(py + k), fs_load(pg + k), sum);
   }
   for (int w = 1; w < lpr; w <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-  if (row < rows && e == 0) {
-    const float x = lse[row];
-    stat[row] = make_float2(x == -INFINITY ? INFINITY : x * FS_LOG2E, sum);
+  if (place < places && e == 0) {
+    const float x = row ? lse[bh * Lq + tok] : -INFINITY;
+    float* to = stat + bh * cross_stat_floats(Lq) + (int64_t)(tok >> 6) * 128 + (tok & 63);
+    to[0] = x == -INFINITY ? -INFINITY : -x * FS_LOG2E;
+    to[64] = row ? -sum : 0.f;
   }
 }
 
@@ -54,11 +56,11 @@ cross_sum_kernel(const float* __restrict__ part, int pieces, int64_t rows, int l
 }
 
 template <typename T>
-int run_delta(fsharp_ctx* ctx, const CrossArgs& a, const void* Y, TensorAddr ay, const void* dY, TensorAddr ady, const float* lse, float2* stat) {
-  const int64_t rows = (int64_t)a.B * a.H * a.Lq, blocks = (rows * (a.dv * (int64_t)sizeof(T) / 16) + 255) / 256;
+int run_delta(fsharp_ctx* ctx, const CrossArgs& a, const void* Y, TensorAddr ay, const void* dY, TensorAddr ady, const float* lse, float* stat) {
+  const int64_t places = (int64_t)a.B * a.H * (((int64_t)a.Lq + 63) / 64 * 64), blocks = (places * (a.dv * (int64_t)sizeof(T) / 16) + 255) / 256;
   if (blocks > 0x7fffffff) return FSHARP_E_SHAPE;
   FS_TIME_BEGIN(ctx, FS_K_CROSS_DELTA);
-  cross_delta_kernel<T><<<(unsigned)blocks, 256, 0, ctx->stream>>>(static_cast<const T*>(Y), ay, static_cast<const T*>(dY), ady, lse, rows,
+  cross_delta_kernel<T><<<(unsigned)blocks, 256, 0, ctx->stream>>>(static_cast<const T*>(Y), ay, static_cast<const T*>(dY), ady, lse, places,
                                                                     a.H, a.Lq, a.dv, stat);
   FS_TIME_END(ctx);
   FS_LAUNCH_CHECK(ctx);
@@ -101,10 +103,10 @@ int check_tensor(const void* p, int dtype, const int64_t s[3]) {
   return FSHARP_OK;
 }
 
-// K or V: the same, and a token stride that tells the keys apart.
-int check_keys(const void* p, int dtype, const int64_t s[3], int Lk) {
+// The same, and a token stride that tells the tokens apart (a tensor map has no other).
+int check_tokens(const void* p, int dtype, const int64_t s[3], int L) {
   FS_TRY(check_tensor(p, dtype, s));
-  return Lk > 1 && s[2] == 0 && (s[0] != 0 || s[1] != 0) ? FSHARP_E_SHAPE : FSHARP_OK;
+  return L > 1 && s[2] == 0 && (s[0] != 0 || s[1] != 0) ? FSHARP_E_SHAPE : FSHARP_OK;
 }
 
 enum Kind { ROWS, FMA, TC };
@@ -130,14 +132,16 @@ Plan plan_forward(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype)
 }
 
 struct GradPlan {
+  bool tc;
   int kv_pieces, q_pieces;
   int64_t stat, kv_floats, q_floats;
 };
 GradPlan plan_backward(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype) {
   GradPlan p = {};
   const int64_t R = (int64_t)dm->H / dm->Hk * dm->Lq, units = (int64_t)dm->B * dm->Hk;
-  fs_cross_fma_grad_pieces(ctx, dm, &p.kv_pieces, &p.q_pieces);
-  p.stat = units * R;
+  p.tc = dtype == FSHARP_BF16 && ctx->impl != FSHARP_IMPL_SIMT && dm->Lk > 0;
+  (p.tc ? fs_tc_cross_grad_pieces : fs_cross_fma_grad_pieces)(ctx, dm, &p.kv_pieces, &p.q_pieces);
+  p.stat = (int64_t)dm->B * dm->H * cross_stat_floats(dm->Lq);
   if (p.kv_pieces > 1) p.kv_floats = p.kv_pieces * units * dm->Lk * (dm->d + dm->dv);
   if (p.q_pieces > 1) p.q_floats = p.q_pieces * units * R * dm->d;
   return p;
@@ -157,7 +161,7 @@ CrossArgs args_of(const fsharp_cross_dims* dm, const void* Q, const void* K, con
 }
 
 int64_t forward_bytes(const Plan& p) { return p.pieces > 1 ? (int64_t)(ws_round(p.o_floats * 4) + ws_round(p.ml * 8)) : 0; }
-int64_t backward_bytes(const GradPlan& p) { return (int64_t)(ws_round(p.stat * 8) + ws_round(p.kv_floats * 4) + ws_round(p.q_floats * 4)); }
+int64_t backward_bytes(const GradPlan& p) { return (int64_t)(ws_round(p.stat * 4) + ws_round(p.kv_floats * 4) + ws_round(p.q_floats * 4)); }
 
 int check_scratch(const void* scratch, int64_t have, int64_t need) {
   if (need == 0) return FSHARP_OK;
@@ -186,8 +190,8 @@ int fsharp_cross_attend(fsharp_ctx* ctx, const void* Q, const void* K, const voi
   if ((int64_t)dims->B * dims->H == 0 || dims->Lq == 0) return FSHARP_OK;
   FS_TRY(check_tensor(Q, dtype, dims->q_stride));
   if (dims->Lk) {                     // (without keys K and V are not read)
-    FS_TRY(check_keys(K, dtype, dims->k_stride, dims->Lk));
-    FS_TRY(check_keys(V, dtype, dims->v_stride, dims->Lk));
+    FS_TRY(check_tokens(K, dtype, dims->k_stride, dims->Lk));
+    FS_TRY(check_tokens(V, dtype, dims->v_stride, dims->Lk));
   }
   FS_TRY(check_tensor(Y, dtype, dims->y_stride));
   const Plan p = plan_forward(ctx, dims, dtype);
@@ -217,14 +221,14 @@ int fsharp_cross_attend_backward(fsharp_ctx* ctx, const void* Q, const void* K, 
   if (dims->mask_stride < 0) return FSHARP_E_BADARG;
   if ((int64_t)dims->B * dims->H == 0) return FSHARP_OK;
   if (dims->Lq == 0) return dims->Lk == 0 ? FSHARP_OK : FSHARP_E_SHAPE;      // no query: nothing to differentiate
-  FS_TRY(check_tensor(Q, dtype, dims->q_stride));
+  FS_TRY(check_tokens(Q, dtype, dims->q_stride, dims->Lq));
   FS_TRY(check_tensor(Y, dtype, dims->y_stride));
-  FS_TRY(check_tensor(dY, dtype, dims->dy_stride));
+  FS_TRY(check_tokens(dY, dtype, dims->dy_stride, dims->Lq));
   FS_TRY(check_tensor(dQ, dtype, dims->dq_stride));
   if (!lse) return FSHARP_E_BADARG;
   if (dims->Lk) {
-    FS_TRY(check_keys(K, dtype, dims->k_stride, dims->Lk));
-    FS_TRY(check_keys(V, dtype, dims->v_stride, dims->Lk));
+    FS_TRY(check_tokens(K, dtype, dims->k_stride, dims->Lk));
+    FS_TRY(check_tokens(V, dtype, dims->v_stride, dims->Lk));
     FS_TRY(check_tensor(dK, dtype, dims->dk_stride));
     FS_TRY(check_tensor(dV, dtype, dims->dv_stride));
   }
@@ -234,7 +238,7 @@ int fsharp_cross_attend_backward(fsharp_ctx* ctx, const void* Q, const void* K, 
   if (!device.ok) return FSHARP_E_CUDA;
   const CrossArgs a = args_of(dims, Q, K, V, key_len, key_mask, scale);
   WsAlloc ws{static_cast<char*>(scratch), 0};
-  float2* stat = ws.take<float2>(p.stat);
+  float* stat = ws.take<float>(p.stat);
   CrossGrad gr;
   gr.dY = dY;
   gr.ady = fs_addr(dims->dy_stride, dims->H, dims->Lq, dims->dv);
@@ -250,7 +254,7 @@ int fsharp_cross_attend_backward(fsharp_ctx* ctx, const void* Q, const void* K, 
   const TensorAddr ay = fs_addr(dims->y_stride, dims->H, dims->Lq, dims->dv);
   const bool f32 = dtype == FSHARP_F32;
   FS_TRY(f32 ? run_delta<float>(ctx, a, Y, ay, dY, gr.ady, lse, stat) : run_delta<__nv_bfloat16>(ctx, a, Y, ay, dY, gr.ady, lse, stat));
-  FS_TRY(fs_cross_fma_grad(ctx, a, dtype, gr));
+  FS_TRY(p.tc ? fs_tc_cross_grad(ctx, a, gr) : fs_cross_fma_grad(ctx, a, dtype, gr));
   const auto sum = f32 ? run_sum<float> : run_sum<__nv_bfloat16>;
   const int64_t keys = (int64_t)a.B * a.Hk * a.Lk;
   if (gr.pkv) {

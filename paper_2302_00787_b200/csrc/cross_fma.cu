@@ -183,10 +183,14 @@ __device__ __forceinline__ void p_ds(float (&p)[4][4], float (&ds)[4][4], const 
 #pragma unroll
     for (int j = 0; j < 4; j++) {
       const bool on = seen[tx + 16 * j];
-      p[i][j] = on ? exp2f(fmaf(p[i][j], c, -st.x)) : 0.f;
-      ds[i][j] = on ? p[i][j] * (ds[i][j] - st.y) * scale : 0.f;
+      p[i][j] = on ? exp2f(fmaf(p[i][j], c, st.x)) : 0.f;
+      ds[i][j] = on ? p[i][j] * (ds[i][j] + st.y) * scale : 0.f;
     }
   }
+}
+
+__device__ __forceinline__ float2 stat_of(const CrossArgs& a, const CrossGrad& gr, int b, int hk, int r) {
+  return r < a.g * a.Lq ? cross_stat(gr.stat, (int64_t)b * a.H + hk * a.g + r / a.Lq, a.Lq, r % a.Lq) : make_float2(-INFINITY, 0.f);
 }
 
 template <int D> constexpr size_t dkv_smem() { return sizeof(float) * (4 * 64 * (D + 4) + 2 * 64 * FM_LP + 3 * 64); }
@@ -214,7 +218,7 @@ cross_dkv_kernel(const __grid_constant__ CrossArgs a, const __grid_constant__ Cr
     __syncthreads();
     load_tile<T, D, 64>(sq, a.d, [&](int r) { return r0 + r < R ? row_of<T>(a.Q, a.aq, b, hk * a.g + (r0 + r) / a.Lq, (r0 + r) % a.Lq) : nullptr; });
     load_tile<T, D, 64>(sg, a.dv, [&](int r) { return r0 + r < R ? row_of<T>(gr.dY, gr.ady, b, hk * a.g + (r0 + r) / a.Lq, (r0 + r) % a.Lq) : nullptr; });
-    if (threadIdx.x < 64) stat[threadIdx.x] = r0 + threadIdx.x < R ? gr.stat[(int64_t)unit * R + r0 + threadIdx.x] : make_float2(INFINITY, 0.f);
+    if (threadIdx.x < 64) stat[threadIdx.x] = stat_of(a, gr, b, hk, r0 + threadIdx.x);
     __syncthreads();
     float p[4][4], ds[4][4];
     p_ds<D>(p, ds, sq, sg, sk, sv, stat, seen, c, a.scale);
@@ -268,7 +272,7 @@ cross_dq_kernel(const __grid_constant__ CrossArgs a, const __grid_constant__ Cro
   const float c = a.scale * FS_LOG2E;
   load_tile<T, D, 64>(sq, a.d, [&](int r) { return r0 + r < R ? row_of<T>(a.Q, a.aq, b, hk * a.g + (r0 + r) / a.Lq, (r0 + r) % a.Lq) : nullptr; });
   load_tile<T, D, 64>(sg, a.dv, [&](int r) { return r0 + r < R ? row_of<T>(gr.dY, gr.ady, b, hk * a.g + (r0 + r) / a.Lq, (r0 + r) % a.Lq) : nullptr; });
-  if (threadIdx.x < 64) stat[threadIdx.x] = r0 + threadIdx.x < R ? gr.stat[(int64_t)unit * R + r0 + threadIdx.x] : make_float2(INFINITY, 0.f);
+  if (threadIdx.x < 64) stat[threadIdx.x] = stat_of(a, gr, b, hk, r0 + threadIdx.x);
   float dq[4][D / 16] = {};
   for (int t = t0; t < t1; t++) {
     const int j0 = t * 64;

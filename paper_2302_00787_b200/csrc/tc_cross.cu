@@ -13,10 +13,12 @@
 // Bound: exponentials (128 x 128 per tile and warpgroup; part of them by a cubic on the multiply-add pipe) and issue slots.
 #include "cross.cuh"
 #include "tc_common.cuh"
+#include "tc_cross.cuh"
 #include "tc_layout.cuh"
 
 using namespace tc;
 using namespace tcl;
+using namespace tcx;
 
 namespace {
 
@@ -37,19 +39,6 @@ struct CxMs {
   int abort_flag;
 };
 static_assert(sizeof(CxMs) <= 512, "misc block");
-
-// max of three that hands NaNs on
-__device__ __forceinline__ float max3n(float a, float b, float c) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-__device__ __forceinline__ void fma2(uint32_t& a, uint32_t& b, float m, float n) {      // (a, b) = (a, b) m + n
-  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
-      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
-      : "+r"(a), "+r"(b)
-      : "f"(m), "f"(n));
-}
 
 template <int D>
 __global__ void __launch_bounds__(CX_T, 1)
@@ -324,6 +313,7 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
               *reinterpret_cast<uint4*>(y + q + k) = make_uint4(pack_bf16(x[k], x[k + 1]), pack_bf16(x[k + 2], x[k + 3]), pack_bf16(x[k + 4], x[k + 5]), pack_bf16(x[k + 6], x[k + 7]));
           }
         }
+        __syncwarp();
       }
       if (r < R) {
         if (part.pieces > 1) part.ml[at] = make_float2(m, sum);
@@ -355,18 +345,18 @@ int launch(fsharp_ctx* ctx, const CUtensorMap& tmK, const CUtensorMap& tmV, cons
 }  // namespace
 
 namespace tchost {
-int make_map_tokens(CUtensorMap* map, const void* base, TensorAddr a, int B, int H, int L, int inner);
+int make_map_rows(CUtensorMap* map, const void* base, TensorAddr a, int B, int H, int L, int inner, int box_rows);
 }
 
-// Keys or values as a tensor map.  A dimension of size one may carry any stride, which nothing reads; one whose entries are all the
+// A tensor as a map of boxes of `rows` tokens.  A dimension of size one may carry any stride, which nothing reads; one whose entries are all the
 // same (stride zero) becomes a dimension of size one.
-int fs_tc_cross_map(CUtensorMap* map, const void* base, TensorAddr t, int B, int H, int L, int inner) {
+int fs_tc_cross_map(CUtensorMap* map, const void* base, TensorAddr t, int B, int H, int L, int inner, int rows) {
   if (t.sh == 0) H = 1;
   if (t.sb == 0) B = 1;
   if (L == 1) t.sl = inner;
   if (H == 1) t.sh = t.sl * L;
   if (B == 1) t.sb = t.sh * H;
-  return tchost::make_map_tokens(map, base, t, B, H, L, inner);
+  return tchost::make_map_rows(map, base, t, B, H, L, inner, rows);
 }
 
 // Pieces that bring the blocks up to one per SM, each with two tiles at least.
@@ -380,7 +370,7 @@ int fs_tc_cross_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm) {
 
 int fs_tc_cross(fsharp_ctx* ctx, const CrossArgs& a, void* Y, TensorAddr ay, float* lse, CrossPart part) {
   CUtensorMap tmK, tmV;
-  FS_TRY(fs_tc_cross_map(&tmK, a.K, a.ak, a.B, a.Hk, a.Lk, a.d));
-  FS_TRY(fs_tc_cross_map(&tmV, a.V, a.av, a.B, a.Hk, a.Lk, a.dv));
+  FS_TRY(fs_tc_cross_map(&tmK, a.K, a.ak, a.B, a.Hk, a.Lk, a.d, TILE));
+  FS_TRY(fs_tc_cross_map(&tmV, a.V, a.av, a.B, a.Hk, a.Lk, a.dv, TILE));
   return a.d > 64 || a.dv > 64 ? launch<128>(ctx, tmK, tmV, a, Y, ay, lse, part) : launch<64>(ctx, tmK, tmV, a, Y, ay, lse, part);
 }

@@ -1,0 +1,512 @@
+// Gradients of the exact cross attention of bf16 tensors on the tensor cores, from P = 2^(x - lse) made again:
+//   dkv   per 128 keys, over the rows in tiles of 64:  S^T = K Q^T, dP^T = V dY^T;  dV += P^T dY, dK += dS^T Q
+//   dq    per 256 rows (128 per warpgroup), over the keys in tiles of 64:  S = Q K^T, dP = dY V^T;  dQ += dS K
+// with dS = P (dP - D); the scores' factor is applied to the sums at the end.  P and dS, rounded to bf16, are operands in tensor
+// memory, where the scores and dP were; thread = key (dkv) or row (dq).  Two kernels that both make P instead of one that adds
+// dQ up in memory with atomics: sums keep a fixed order, and the exponentials, made twice, hide under the products.
+// Two warpgroups take the tiles in turn (dkv), so that one's products run while the other is at its exponentials; in dq each has
+// rows of its own and they share every K and V tile (up to 128 rows: tiles in turn, two partial dQ that meet at the end).
+// Bound: the tensor pipe (four products of 128 x 64 x d per tile in dkv, three in dq; with N = 64 the two that read both operands
+// from shared memory are bound by its 128 bytes per clock) and the exponentials beside it.
+#include "cross.cuh"
+#include "tc_common.cuh"
+#include "tc_cross.cuh"
+#include "tc_layout.cuh"
+
+using namespace tc;
+using namespace tcl;
+using namespace tcx;
+
+int fs_tc_cross_map(CUtensorMap* map, const void* base, TensorAddr t, int B, int H, int L, int inner, int rows);
+
+namespace {
+
+constexpr int CG_WARPS = 8, CGW_TMA = 8, CGW_MMA = 9, CG_T = 384;      // (warps 10, 11 only hand their registers over)
+constexpr int HALF = 64;                                                // rows (dkv) or keys (dq) of a walked tile
+constexpr uint32_t HALF_BYTES = 8192;                                   // 64 rows x 128 bytes
+constexpr uint32_t CG_TMEM = 512, CG_SUM = 256;                         // two pairs (S, dP) of 64 columns each, then the sums
+
+// The exponentials of 64 columns, those of every other four by the cubic, and dS; packed into the places of the first 32 registers.
+// (nl, nd): -lse log2(e) and -D of the columns (dkv).
+__device__ __forceinline__ void exps2(uint32_t& x, uint32_t& y, bool cubic) {
+  if (cubic) exp2_poly2(x, y);
+  else { x = __float_as_uint(ex2(__uint_as_float(x))); y = __float_as_uint(ex2(__uint_as_float(y))); }
+}
+
+// ------------------------------------------------------------------------------------------ dK, dV
+template <int D>
+struct KvSm {
+  static constexpr int PANELS = D / 64, NS = D == 64 ? 6 : 4;
+  static constexpr uint32_t K = 0, V = PANELS * TILE_BYTES, RING = 2 * PANELS * TILE_BYTES, SLOT = PANELS * HALF_BYTES, STAGE = 2 * SLOT;
+  static constexpr uint32_t STAT = RING + NS * STAGE, MISC = STAT + NS * 512, TOTAL = MISC + 512;
+  static_assert(TOTAL + 1024 <= 232448, "shared memory budget");
+};
+struct KvMs {
+  uint64_t full[8], empty[8], sp_full[2], ready[2], kv_full, done;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+static_assert(sizeof(KvMs) <= 512, "misc block");
+
+template <int D>
+__global__ void __launch_bounds__(CG_T, 1)
+tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmG, const __grid_constant__ CUtensorMap tmK,
+                    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CrossArgs a, const __grid_constant__ CrossGrad gr,
+                    int* __restrict__ status) {
+  using Sm = KvSm<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  KvMs* misc = reinterpret_cast<KvMs*>(sm + Sm::MISC);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* abortp = &misc->abort_flag;
+  const int unit = blockIdx.y, piece = blockIdx.x % gr.kv_pieces, j0 = (int)(blockIdx.x / gr.kv_pieces) * TILE;
+  const int b = unit / a.Hk, hk = unit % a.Hk, n = cross_keys(a, b);
+  // row tiles: those of the first query head of the group, of the second, ...
+  const int per = (a.Lq + HALF - 1) / HALF;
+  const int64_t tiles = j0 < n ? (int64_t)a.g * per : 0;
+  const int t0 = (int)(tiles * piece / gr.kv_pieces), items = (int)(tiles * (piece + 1) / gr.kv_pieces) - t0;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < Sm::NS; i++) { mbar_init(&misc->full[i], 1); mbar_init(&misc->empty[i], 1); }
+    for (int w = 0; w < 2; w++) { mbar_init(&misc->sp_full[w], 1); mbar_init(&misc->ready[w], 4); }
+    mbar_init(&misc->kv_full, 1);
+    mbar_init(&misc->done, 1);
+    misc->abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == CGW_MMA) {
+    tmem_alloc(&misc->tmem_base, CG_TMEM);
+    tmem_relinquish();
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  tcgen05_fence_after();
+  const uint32_t tmem = misc->tmem_base;
+  const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;
+
+  if (warp >= CG_WARPS) regs_release<REGS_PRODUCER>();
+  if (warp == CGW_TMA) {
+    if (lane == 0 && items > 0) {
+      prefetch_tmap(&tmQ); prefetch_tmap(&tmG); prefetch_tmap(&tmK); prefetch_tmap(&tmV);
+      mbar_expect_tx(&misc->kv_full, (kp + vp) * TILE_BYTES);
+      for (int p = 0; p < kp; p++) tma_load_4d(sm + Sm::K + p * TILE_BYTES, &tmK, &misc->kv_full, p * 64, j0, a.ak.sh ? hk : 0, a.ak.sb ? b : 0);
+      for (int p = 0; p < vp; p++) tma_load_4d(sm + Sm::V + p * TILE_BYTES, &tmV, &misc->kv_full, p * 64, j0, a.av.sh ? hk : 0, a.av.sb ? b : 0);
+      int i = 0;
+      for (; i < items; i++) {
+        const int s = i % Sm::NS, h = hk * a.g + (t0 + i) / per, t = (t0 + i) % per;
+        if (!mbar_wait(&misc->empty[s], ((i / Sm::NS) & 1) ^ 1, abortp, status)) break;
+        uint8_t* base = sm + Sm::RING + s * Sm::STAGE;
+        mbar_expect_tx(&misc->full[s], (kp + vp) * HALF_BYTES + 512);
+        for (int p = 0; p < kp; p++) tma_load_4d(base + p * HALF_BYTES, &tmQ, &misc->full[s], p * 64, t * HALF, a.aq.sh ? h : 0, a.aq.sb ? b : 0);
+        for (int p = 0; p < vp; p++)
+          tma_load_4d(base + Sm::SLOT + p * HALF_BYTES, &tmG, &misc->full[s], p * 64, t * HALF, gr.ady.sh ? h : 0, gr.ady.sb ? b : 0);
+        bulk_load(sm + Sm::STAT + s * 512, gr.stat + ((int64_t)b * a.H + h) * cross_stat_floats(a.Lq) + (int64_t)t * 128, 512, &misc->full[s]);
+      }
+      // no copy of this block may still be in flight when it exits
+      mbar_wait(&misc->kv_full, 0, abortp, status, false);
+      for (int k = max(0, i - Sm::NS); k < i; k++) mbar_wait(&misc->full[k % Sm::NS], (k / Sm::NS) & 1, abortp, status, false);
+    }
+  } else if (warp == CGW_MMA) {
+    constexpr uint32_t ID_S = idesc_bf16(128, HALF, 0, 0);
+    const uint32_t ID_V = idesc_bf16(128, a.dv, 0, 1), ID_K = idesc_bf16(128, a.d, 0, 1);
+    const uint32_t sR = smem_u32(sm + Sm::RING);
+    const uint64_t dK = smem_desc(smem_u32(sm + Sm::K), 16, 1024, SWZ_128B), dV = smem_desc(smem_u32(sm + Sm::V), 16, 1024, SWZ_128B);
+    const int ks = a.d / 16, vs = a.dv / 16;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abortp, status)) != 0; };
+    auto issue_sp = [&](int i) {                       // S^T and dP^T of tile i
+      const int s = i % Sm::NS, w = i & 1;
+      if (!wait(&misc->full[s], (i / Sm::NS) & 1)) return false;
+      tcgen05_fence_after();
+      const uint64_t dQ = smem_desc(sR + s * Sm::STAGE, 16, 1024, SWZ_128B), dG = smem_desc(sR + s * Sm::STAGE + Sm::SLOT, 16, 1024, SWZ_128B);
+      if (elect_one()) {
+        for (int k = 0; k < ks; k++)
+          mma_bf16(tmem + w * 128, desc_advance(dK, (k >> 2) * TILE_BYTES + (k & 3) * 32), desc_advance(dQ, (k >> 2) * HALF_BYTES + (k & 3) * 32), ID_S, k > 0);
+        for (int k = 0; k < vs; k++)
+          mma_bf16(tmem + w * 128 + 64, desc_advance(dV, (k >> 2) * TILE_BYTES + (k & 3) * 32), desc_advance(dG, (k >> 2) * HALF_BYTES + (k & 3) * 32), ID_S, k > 0);
+        mma_commit(&misc->sp_full[w]);
+      }
+      __syncwarp();
+      return true;
+    };
+    bool ok = items > 0 && wait(&misc->kv_full, 0) && issue_sp(0) && (items < 2 || issue_sp(1));
+    for (int i = 0; i < items && ok; i++) {
+      const int s = i % Sm::NS, w = i & 1;
+      if (!(ok = wait(&misc->ready[w], (i >> 1) & 1))) break;
+      tcgen05_fence_after();
+      // Q and dY again, now with their rows as the contraction: panels of 64 columns, 16 rows of 128 bytes per step
+      const uint64_t dQ = smem_desc(sR + s * Sm::STAGE, HALF_BYTES, 1024, SWZ_128B), dG = smem_desc(sR + s * Sm::STAGE + Sm::SLOT, HALF_BYTES, 1024, SWZ_128B);
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < 4; k++) mma_bf16_ta(tmem + CG_SUM, tmem + w * 128 + 8 * k, desc_advance(dG, k * 2048), ID_V, i > 0 || k > 0);
+#pragma unroll
+        for (int k = 0; k < 4; k++) mma_bf16_ta(tmem + CG_SUM + D, tmem + w * 128 + 64 + 8 * k, desc_advance(dQ, k * 2048), ID_K, i > 0 || k > 0);
+        mma_commit(&misc->empty[s]);
+        if (i == items - 1) mma_commit(&misc->done);
+      }
+      __syncwarp();
+      if (i + 2 < items) ok = issue_sp(i + 2);
+    }
+  } else if (warp < CG_WARPS) {
+    regs_acquire<REGS_EPILOGUE>();
+    const int w = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), tS = lanes + w * 128, tP = tS + 64;
+    const float c = a.scale * FS_LOG2E;
+    bool ok = true;
+    for (int i = w; i < items; i += 2) {
+      const int s = i % Sm::NS;
+      // (what a hidden key holds, NaNs too, stays in its own row of S^T, dP^T and of the sums, and is dropped at the end)
+      ok = __all_sync(0xffffffffu, mbar_wait(&misc->sp_full[w], (i >> 1) & 1, abortp, status, false) &&
+                                       mbar_wait(&misc->full[s], (i / Sm::NS) & 1, abortp, status, false));
+      if (!ok) break;
+      tcgen05_fence_after();
+      const float* st = reinterpret_cast<const float*>(sm + Sm::STAT + s * 512);
+      uint32_t x[64], g[64];
+#pragma unroll
+      for (int q = 0; q < 4; q++) tmem_ld16(tS + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(x + 16 * q));
+#pragma unroll
+      for (int q = 0; q < 4; q++) tmem_ld16(tP + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(g + 16 * q));
+      tmem_wait_ld();
+#pragma unroll
+      for (int q = 0; q < 64; q += 32) {
+        uint32_t o[16], u[16];
+#pragma unroll
+        for (int k = 0; k < 32; k += 4) {
+          const float4 nl = *reinterpret_cast<const float4*>(st + q + k), nd = *reinterpret_cast<const float4*>(st + 64 + q + k);
+          uint32_t *xp = x + q + k, *gp = g + q + k;
+          fma2v(xp[0], xp[1], c, nl.x, nl.y);
+          fma2v(xp[2], xp[3], c, nl.z, nl.w);
+          exps2(xp[0], xp[1], false);
+          exps2(xp[2], xp[3], true);
+          addmul2(gp[0], gp[1], nd.x, nd.y, xp[0], xp[1]);
+          addmul2(gp[2], gp[3], nd.z, nd.w, xp[2], xp[3]);
+          o[k / 2] = pack_bf16(__uint_as_float(xp[0]), __uint_as_float(xp[1]));
+          o[k / 2 + 1] = pack_bf16(__uint_as_float(xp[2]), __uint_as_float(xp[3]));
+          u[k / 2] = pack_bf16(__uint_as_float(gp[0]), __uint_as_float(gp[1]));
+          u[k / 2 + 1] = pack_bf16(__uint_as_float(gp[2]), __uint_as_float(gp[3]));
+        }
+        tmem_st16(tS + q / 2, o);
+        tmem_st16(tP + q / 2, u);
+      }
+      tmem_wait_st();
+      tcgen05_fence_before();
+      mbar_arrive_warp(&misc->ready[w], lane);
+    }
+    if (ok && items > 0) ok = __all_sync(0xffffffffu, mbar_wait(&misc->done, 0, abortp, status, false));
+    tcgen05_fence_after();
+    if (ok) {
+      // the first warpgroup writes dV, the second dK
+      const int j = j0 + row, width = w ? a.d : a.dv;
+      const bool on = cross_seen(a, b, j, n);
+      const float f = w ? a.scale : 1.f;
+      const TensorAddr to = w ? gr.adk : gr.adv;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(w ? gr.dK : gr.dV) + b * to.sb + hk * to.sh + j * to.sl;
+      float* part = gr.pkv + (((int64_t)piece * a.B * a.Hk + unit) * a.Lk + j) * (a.d + a.dv) + (w ? 0 : a.d);
+      for (int q = 0; q < width; q += 16) {
+        uint32_t t[16] = {};
+        if (items > 0) {
+          tmem_ld16(lanes + CG_SUM + w * D + q, t);
+          tmem_wait_ld();
+        }
+        float x[16];
+#pragma unroll
+        for (int k = 0; k < 16; k++) x[k] = on ? __uint_as_float(t[k]) * f : 0.f;
+        if (j < a.Lk && gr.pkv) {
+#pragma unroll
+          for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(part + q + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+        } else if (j < a.Lk) {
+#pragma unroll
+          for (int k = 0; k < 16; k += 8)
+            *reinterpret_cast<uint4*>(out + q + k) = make_uint4(pack_bf16(x[k], x[k + 1]), pack_bf16(x[k + 2], x[k + 3]), pack_bf16(x[k + 4], x[k + 5]), pack_bf16(x[k + 6], x[k + 7]));
+        }
+        __syncwarp();
+      }
+    }
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  if (warp == CGW_MMA) {
+    tcgen05_fence_after();
+    tmem_dealloc(tmem, CG_TMEM);
+  }
+}
+
+// ------------------------------------------------------------------------------------------ dQ
+template <int D>
+struct DqSm {
+  static constexpr int PANELS = D / 64, NS = D == 64 ? 6 : 3;
+  static constexpr uint32_t BIG = PANELS * TILE_BYTES, Q = 0, G = 2 * BIG, RING = 4 * BIG, SLOT = PANELS * HALF_BYTES, STAGE = 2 * SLOT;
+  static constexpr uint32_t MISC = RING + NS * STAGE, TOTAL = MISC + 512;
+  static_assert(TOTAL + 1024 <= 232448, "shared memory budget");
+  static_assert(4 * BIG >= 128 * (D + 1) * 4, "the warpgroups' exchange");
+};
+struct DqMs {
+  uint64_t full[8], empty[8], sp_full[2], ready[2], done[2], q_ready;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+static_assert(sizeof(DqMs) <= 512, "misc block");
+
+template <int D>
+__global__ void __launch_bounds__(CG_T, 1)
+tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CrossArgs a,
+                   const __grid_constant__ CrossGrad gr, int* __restrict__ status) {
+  using Sm = DqSm<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  DqMs* misc = reinterpret_cast<DqMs*>(sm + Sm::MISC);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* abortp = &misc->abort_flag;
+  const int unit = blockIdx.y, piece = blockIdx.x % gr.q_pieces, r0 = (int)(blockIdx.x / gr.q_pieces) * 256;
+  const int b = unit / a.Hk, hk = unit % a.Hk, R = a.g * a.Lq;
+  const int n = cross_keys(a, b), tiles = (n + HALF - 1) / HALF;
+  const int t0 = (int)((int64_t)tiles * piece / gr.q_pieces), nt = (int)((int64_t)tiles * (piece + 1) / gr.q_pieces) - t0;
+  const bool both = R - r0 > TILE;                     // each warpgroup has rows of its own
+  const int items = both ? 2 * nt : nt;                // item i: warpgroup i & 1, tile i / 2 or i
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < Sm::NS; i++) { mbar_init(&misc->full[i], 1); mbar_init(&misc->empty[i], 1); }
+    for (int w = 0; w < 2; w++) { mbar_init(&misc->sp_full[w], 1); mbar_init(&misc->ready[w], 4); mbar_init(&misc->done[w], 1); }
+    mbar_init(&misc->q_ready, CG_WARPS);
+    misc->abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == CGW_MMA) {
+    tmem_alloc(&misc->tmem_base, CG_TMEM);
+    tmem_relinquish();
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  tcgen05_fence_after();
+  const uint32_t tmem = misc->tmem_base;
+  const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;
+
+  if (warp >= CG_WARPS) regs_release<REGS_PRODUCER>();
+  if (warp == CGW_TMA) {
+    if (lane == 0) {
+      prefetch_tmap(&tmK); prefetch_tmap(&tmV);
+      int i = 0;
+      for (; i < nt; i++) {
+        const int s = i % Sm::NS, tok = (t0 + i) * HALF;
+        if (!mbar_wait(&misc->empty[s], ((i / Sm::NS) & 1) ^ 1, abortp, status)) break;
+        uint8_t* base = sm + Sm::RING + s * Sm::STAGE;
+        mbar_expect_tx(&misc->full[s], (kp + vp) * HALF_BYTES);
+        for (int p = 0; p < kp; p++) tma_load_4d(base + p * HALF_BYTES, &tmK, &misc->full[s], p * 64, tok, a.ak.sh ? hk : 0, a.ak.sb ? b : 0);
+        for (int p = 0; p < vp; p++) tma_load_4d(base + Sm::SLOT + p * HALF_BYTES, &tmV, &misc->full[s], p * 64, tok, a.av.sh ? hk : 0, a.av.sb ? b : 0);
+      }
+      // no copy of this block may still be in flight when it exits
+      for (int k = max(0, i - Sm::NS); k < i; k++) mbar_wait(&misc->full[k % Sm::NS], (k / Sm::NS) & 1, abortp, status, false);
+    }
+  } else if (warp == CGW_MMA) {
+    constexpr uint32_t ID_S = idesc_bf16(128, HALF, 0, 0);
+    const uint32_t ID_Q = idesc_bf16(128, a.d, 0, 1);
+    const uint32_t sR = smem_u32(sm + Sm::RING), sQ = smem_u32(sm + Sm::Q), sG = smem_u32(sm + Sm::G);
+    const int ks = a.d / 16, vs = a.dv / 16;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abortp, status)) != 0; };
+    auto issue_sp = [&](int i) {                       // S and dP of item i
+      const int w = i & 1, t = both ? i >> 1 : i, s = t % Sm::NS;
+      if (!wait(&misc->full[s], (t / Sm::NS) & 1)) return false;
+      tcgen05_fence_after();
+      const uint64_t dK = smem_desc(sR + s * Sm::STAGE, 16, 1024, SWZ_128B), dV = smem_desc(sR + s * Sm::STAGE + Sm::SLOT, 16, 1024, SWZ_128B);
+      const uint64_t dQ = smem_desc(sQ + (both ? w : 0) * Sm::BIG, 16, 1024, SWZ_128B), dG = smem_desc(sG + (both ? w : 0) * Sm::BIG, 16, 1024, SWZ_128B);
+      if (elect_one()) {
+        for (int k = 0; k < ks; k++)
+          mma_bf16(tmem + w * 128, desc_advance(dQ, (k >> 2) * TILE_BYTES + (k & 3) * 32), desc_advance(dK, (k >> 2) * HALF_BYTES + (k & 3) * 32), ID_S, k > 0);
+        for (int k = 0; k < vs; k++)
+          mma_bf16(tmem + w * 128 + 64, desc_advance(dG, (k >> 2) * TILE_BYTES + (k & 3) * 32), desc_advance(dV, (k >> 2) * HALF_BYTES + (k & 3) * 32), ID_S, k > 0);
+        mma_commit(&misc->sp_full[w]);
+      }
+      __syncwarp();
+      return true;
+    };
+    bool ok = nt > 0 && wait(&misc->q_ready, 0);
+    if (ok) {
+      tcgen05_fence_after();
+      ok = issue_sp(0) && (items < 2 || issue_sp(1));
+    }
+    for (int i = 0; i < items && ok; i++) {
+      const int w = i & 1, t = both ? i >> 1 : i, s = t % Sm::NS;
+      if (!(ok = wait(&misc->ready[w], (i >> 1) & 1))) break;
+      tcgen05_fence_after();
+      const uint64_t dK = smem_desc(sR + s * Sm::STAGE, HALF_BYTES, 1024, SWZ_128B);      // its keys as the contraction
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < 4; k++) mma_bf16_ta(tmem + CG_SUM + w * 128, tmem + w * 128 + 8 * k, desc_advance(dK, k * 2048), ID_Q, i > 1 || k > 0);
+        if (!both || w) mma_commit(&misc->empty[s]);
+        if (i + 2 >= items) mma_commit(&misc->done[w]);
+      }
+      __syncwarp();
+      if (i + 2 < items) ok = issue_sp(i + 2);
+    }
+  } else if (warp < CG_WARPS) {
+    regs_acquire<REGS_EPILOGUE>();
+    const int w = warp >> 2, row = (warp & 3) * 32 + lane;
+    {
+      // the block's rows of Q and dY into shared memory, rows and columns that there are none of as zeros
+      constexpr int CH = D / 8;
+      const int rows = both ? 256 : 128;
+      for (int i = threadIdx.x; i < 2 * rows * CH; i += 256) {
+        const int which = i >= rows * CH, k = i - which * rows * CH, rr = k / CH, ch = k % CH, r = r0 + rr;
+        const TensorAddr t = which ? gr.ady : a.aq;
+        const __nv_bfloat16* X = static_cast<const __nv_bfloat16*>(which ? gr.dY : a.Q) + b * t.sb;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (r < R && ch * 8 < (which ? a.dv : a.d)) x = *reinterpret_cast<const uint4*>(X + (int64_t)(hk * a.g + r / a.Lq) * t.sh + (int64_t)(r % a.Lq) * t.sl + ch * 8);
+        *reinterpret_cast<uint4*>(sm + (which ? Sm::G : Sm::Q) + (rr >> 7) * Sm::BIG + (ch >> 3) * TILE_BYTES + sw128_offset(rr & 127, (ch & 7) * 8)) = x;
+      }
+      fence_proxy_async_smem();
+      mbar_arrive_warp(&misc->q_ready, lane);
+    }
+    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), tS = lanes + w * 128, tP = tS + 64, tQ = lanes + CG_SUM + w * 128;
+    const int first = r0 + (both ? w * TILE : 0), r = first + row;
+    const bool idle = first + (warp & 3) * 32 >= R;
+    const int mine = both ? nt : (nt + 1 - w) / 2;
+    const float c = a.scale * FS_LOG2E;
+    const float2 st = r < R ? cross_stat(gr.stat, (int64_t)b * a.H + hk * a.g + r / a.Lq, a.Lq, r % a.Lq) : make_float2(-INFINITY, 0.f);
+    bool ok = true;
+    for (int i = 0; i < mine; i++) {
+      const int t = both ? i : 2 * i + w, jj = (t0 + t) * HALF, s = t % Sm::NS;
+      ok = __all_sync(0xffffffffu, mbar_wait(&misc->sp_full[w], i & 1, abortp, status, false) &&
+                                       mbar_wait(&misc->full[s], (t / Sm::NS) & 1, abortp, status, false));
+      if (!ok) break;
+      tcgen05_fence_after();
+      uint32_t seen[2] = {~0u, ~0u};
+      if (a.key_mask != nullptr || jj + HALF > n) {
+#pragma unroll
+        for (int q = 0; q < 2; q++) seen[q] = __ballot_sync(0xffffffffu, cross_seen(a, b, jj + q * 32 + lane, n));
+        // a hidden key's K becomes zeros (it may hold anything) before dS multiplies it; a warp does 16 of the 64 keys.  The other
+        // warpgroup's scores of the same key, made before or after, are dropped like this one's
+        if ((!both || w == 0) && lane < 16) {
+          const int key = (warp & 3) * 16 + lane;
+          if (!(seen[key >> 5] >> (key & 31) & 1u))
+            for (int p = 0; p < kp; p++)
+              for (int k = 0; k < 8; k++)
+                *reinterpret_cast<uint4*>(sm + Sm::RING + s * Sm::STAGE + p * HALF_BYTES + key * 128 + k * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_smem();
+      }
+      if (!idle) {
+        uint32_t x[64], g[64];
+#pragma unroll
+        for (int q = 0; q < 4; q++) tmem_ld16(tS + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(x + 16 * q));
+#pragma unroll
+        for (int q = 0; q < 4; q++) tmem_ld16(tP + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(g + 16 * q));
+        tmem_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 64; k += 4) {
+          fma2(x[k], x[k + 1], c, st.x);
+          fma2(x[k + 2], x[k + 3], c, st.x);
+          exps2(x[k], x[k + 1], false);
+          exps2(x[k + 2], x[k + 3], true);
+          addmul2(g[k], g[k + 1], st.y, st.y, x[k], x[k + 1]);
+          addmul2(g[k + 2], g[k + 3], st.y, st.y, x[k + 2], x[k + 3]);
+        }
+        if ((seen[0] & seen[1]) != ~0u) {
+#pragma unroll
+          for (int k = 0; k < 64; k++) g[k] = (seen[k >> 5] >> (k & 31)) & 1u ? g[k] : 0u;
+        }
+#pragma unroll
+        for (int q = 0; q < 64; q += 32) {
+          uint32_t u[16];
+#pragma unroll
+          for (int k = 0; k < 16; k++) u[k] = pack_bf16(__uint_as_float(g[q + 2 * k]), __uint_as_float(g[q + 2 * k + 1]));
+          tmem_st16(tS + q / 2, u);
+        }
+        tmem_wait_st();
+      }
+      tcgen05_fence_before();
+      mbar_arrive_warp(&misc->ready[w], lane);
+    }
+    if (ok && mine > 0) ok = mbar_wait(&misc->done[w], 0, abortp, status, false);
+    if (ok && !both && (nt + w) / 2 > 0) ok = mbar_wait(&misc->done[w ^ 1], 0, abortp, status, false);
+    ok = __all_sync(0xffffffffu, ok);
+    tcgen05_fence_after();
+    // (every warp comes to the barrier below, also after a wait that ran out; the exchange lies where Q and dY were)
+    float* xo = reinterpret_cast<float*>(sm + Sm::Q);
+    if (!both) {
+      if (w == 1 && ok)
+        for (int q = 0; q < a.d; q += 16) {
+          uint32_t o[16] = {};
+          if (mine > 0) {
+            tmem_ld16(tQ + q, o);
+            tmem_wait_ld();
+          }
+#pragma unroll
+          for (int k = 0; k < 16; k++) xo[row * (D + 1) + q + k] = __uint_as_float(o[k]);
+        }
+      named_bar_sync(3, 256);
+    }
+    if ((both || w == 0) && ok) {
+      const int h = hk * a.g + r / a.Lq, tok = r % a.Lq;
+      float* part = gr.pq + (((int64_t)piece * a.B * a.Hk + unit) * R + r) * a.d;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(gr.dQ) + b * gr.adq.sb + h * gr.adq.sh + tok * gr.adq.sl;
+      for (int q = 0; q < a.d; q += 16) {
+        uint32_t o[16] = {};
+        if (mine > 0) {
+          tmem_ld16(tQ + q, o);
+          tmem_wait_ld();
+        }
+        float x[16];
+#pragma unroll
+        for (int k = 0; k < 16; k++) x[k] = a.scale * (__uint_as_float(o[k]) + (both ? 0.f : xo[row * (D + 1) + q + k]));
+        if (r < R && gr.pq) {
+#pragma unroll
+          for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(part + q + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+        } else if (r < R) {
+#pragma unroll
+          for (int k = 0; k < 16; k += 8)
+            *reinterpret_cast<uint4*>(out + q + k) = make_uint4(pack_bf16(x[k], x[k + 1]), pack_bf16(x[k + 2], x[k + 3]), pack_bf16(x[k + 4], x[k + 5]), pack_bf16(x[k + 6], x[k + 7]));
+        }
+        __syncwarp();
+      }
+    }
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  if (warp == CGW_MMA) {
+    tcgen05_fence_after();
+    tmem_dealloc(tmem, CG_TMEM);
+  }
+}
+
+template <int D>
+int launch(fsharp_ctx* ctx, const CrossArgs& a, const CrossGrad& gr) {
+  const int64_t gk = ((int64_t)a.Lk + TILE - 1) / TILE * gr.kv_pieces, gq = ((int64_t)a.g * a.Lq + 255) / 256 * gr.q_pieces;
+  if (gk > 0x7fffffff || gq > 0x7fffffff) return FSHARP_E_SHAPE;
+  CUtensorMap tmQ, tmG, tmK, tmV, tmK64, tmV64;
+  FS_TRY(fs_tc_cross_map(&tmQ, a.Q, a.aq, a.B, a.H, a.Lq, a.d, HALF));
+  FS_TRY(fs_tc_cross_map(&tmG, gr.dY, gr.ady, a.B, a.H, a.Lq, a.dv, HALF));
+  FS_TRY(fs_tc_cross_map(&tmK, a.K, a.ak, a.B, a.Hk, a.Lk, a.d, TILE));
+  FS_TRY(fs_tc_cross_map(&tmV, a.V, a.av, a.B, a.Hk, a.Lk, a.dv, TILE));
+  FS_TRY(fs_tc_cross_map(&tmK64, a.K, a.ak, a.B, a.Hk, a.Lk, a.d, HALF));
+  FS_TRY(fs_tc_cross_map(&tmV64, a.V, a.av, a.B, a.Hk, a.Lk, a.dv, HALF));
+  FS_CUDA_OK(fs_allow_smem(tc_cross_dkv_kernel<D>));
+  FS_CUDA_OK(fs_allow_smem(tc_cross_dq_kernel<D>));
+  FS_TIME_BEGIN(ctx, FS_K_TC_CROSS_DKV);
+  tc_cross_dkv_kernel<D><<<dim3((unsigned)gk, (unsigned)(a.B * a.Hk)), CG_T, KvSm<D>::TOTAL + 1024, ctx->stream>>>(tmQ, tmG, tmK, tmV, a, gr, ctx->d_status);
+  FS_TIME_END(ctx);
+  FS_LAUNCH_CHECK(ctx);
+  FS_TIME_BEGIN(ctx, FS_K_TC_CROSS_DQ);
+  tc_cross_dq_kernel<D><<<dim3((unsigned)gq, (unsigned)(a.B * a.Hk)), CG_T, DqSm<D>::TOTAL + 1024, ctx->stream>>>(tmK64, tmV64, a, gr, ctx->d_status);
+  FS_TIME_END(ctx);
+  FS_LAUNCH_CHECK(ctx);
+  return FSHARP_OK;
+}
+
+// Pieces that bring `blocks` blocks up to one per SM, each with four tiles at least.
+int pieces_for(const fsharp_ctx* ctx, int64_t blocks, int64_t tiles) {
+  int64_t p = ctx->sm_count / blocks;
+  if (p > tiles / 4) p = tiles / 4;
+  if (p > 64) p = 64;
+  return p < 1 ? 1 : (int)p;
+}
+
+}  // namespace
+
+void fs_tc_cross_grad_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int* kv_pieces, int* q_pieces) {
+  const int64_t g = dm->H / dm->Hk, units = (int64_t)dm->B * dm->Hk;
+  *kv_pieces = pieces_for(ctx, units * (((int64_t)dm->Lk + TILE - 1) / TILE), g * (((int64_t)dm->Lq + HALF - 1) / HALF));
+  *q_pieces = pieces_for(ctx, units * ((g * dm->Lq + 255) / 256), ((int64_t)dm->Lk + HALF - 1) / HALF);
+}
+
+int fs_tc_cross_grad(fsharp_ctx* ctx, const CrossArgs& a, const CrossGrad& gr) {
+  return a.d > 64 || a.dv > 64 ? launch<128>(ctx, a, gr) : launch<64>(ctx, a, gr);
+}
