@@ -321,11 +321,10 @@ int fsharp_rotate(fsharp_ctx* ctx, const void* Q, const void* K, const int64_t* 
  * scratch: device memory of at least fsharp_cross_scratch_bytes() bytes (16-byte aligned; may be NULL where that is 0),
  * used while the call's work is on the stream and not read before it is written.  It is the caller's, not the context's,
  * so that captured graphs and calls on several streams can each have their own; a graph keeps the pointer.
- * bf16 runs on the tensor cores (fewer than FSHARP_CROSS_FEW_ROWS query rows per key head: multiply-add kernels that
- * stream K and V), fp32 on the multiply-add pipe in fp32 throughout.  FSHARP_IMPL_SIMT forces the multiply-add kernels;
+ * bf16 runs on the tensor cores (one query row per key head, forward: a multiply-add kernel that streams K and V), fp32 on
+ * the multiply-add pipe in fp32 throughout.  FSHARP_IMPL_SIMT forces the multiply-add kernels;
  * FSHARP_IMPL_TENSOR refuses fp32 (FSHARP_E_SHAPE).  B * Hk <= 65535.  Strides of zero (one entry for a whole dimension)
  * are allowed, but not for the tokens of K, V and, backward, Q and dY (FSHARP_E_SHAPE), and never in what is written. */
-#define FSHARP_CROSS_FEW_ROWS 5
 typedef struct {
   int32_t B, H, Hk, Lq, Lk, d, dv;
   int64_t q_stride[3], k_stride[3], v_stride[3], y_stride[3];         /* element strides (batch, head, token) */

@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -104,11 +105,11 @@ def load_library() -> C.CDLL:
         "fsharp_attend_with_state": (i32, [vp, vp, vp, vp, vp, vp, dims_p, i32, i32, f32, vp, vp, i32, vp]),
         "fsharp_forward_host": (i32, [vp, vp, vp, vp, vp, dims_p, i32, i32, i32, i32, f32, vp]),
         "fsharp_pair_estimate": (i32, [vp, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp]),
-        "fsharp_rotate": (i32, [vp, vp, vp, vp, i64, i64, C.POINTER(fsharp_rope), C.POINTER(fsharp_rotate_dims), i32, i32, vp,
+        "fsharp_rotate": (i32, [vp, vp, vp, vp, i64, i64, C.POINTER(fsharp_rope), vp, i32, i32, vp,
                                 vp]),
-        "fsharp_cross_scratch_bytes": (i64, [vp, C.POINTER(fsharp_cross_dims), i32, i32]),
-        "fsharp_cross_attend": (i32, [vp, vp, vp, vp, vp, vp, C.POINTER(fsharp_cross_dims), i32, f32, vp, vp, vp, i64]),
-        "fsharp_cross_attend_backward": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, vp, C.POINTER(fsharp_cross_dims), i32, f32, vp,
+        "fsharp_cross_scratch_bytes": (i64, [vp, vp, i32, i32]),
+        "fsharp_cross_attend": (i32, [vp, vp, vp, vp, vp, vp, vp, i32, f32, vp, vp, vp, i64]),
+        "fsharp_cross_attend_backward": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, f32, vp,
                                                vp, vp, vp, i64]),
         "fsharp_set_timing": (i32, [vp, i32]),
         "fsharp_selftest_bounded_wait": (i32, [vp, i32]),
@@ -157,30 +158,40 @@ def _strides(t: torch.Tensor):
     return (C.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
 
 
-def _readable(t: torch.Tensor) -> torch.Tensor:
-    """`t`, or a dense copy where its strides cannot be told to the library: a tensor broadcast along every dimension
-    (three zeros mean dense there) or along its tokens, rows or a start that are not 16-byte aligned, a last dimension with gaps."""
-    if t.dim() != 4:
-        raise ValueError("expected a [B, H, L, inner] tensor")
-    es = t.element_size()
-    strides = [s for s, n in zip(t.stride()[:3], t.shape[:3]) if n > 1]
-    if (t.shape[3] > 1 and t.stride(3) != 1) or (strides and not any(strides)) or any(s * es % 16 for s in strides) \
-            or (t.shape[2] > 1 and t.stride(2) == 0) or t.data_ptr() % 16:
-        return t.contiguous() if not t.is_contiguous() else t.clone()
-    return t
+_INNER_ONLY = {torch.float32: 3, torch.bfloat16: 7}      # element strides are multiples of 16 bytes: these bits are zero
+_CROSS_DIMS = struct.Struct("=7i4x25q")                  # fsharp_cross_dims, packed
+_ROTATE_DIMS = struct.Struct("=5i4x12q")                 # fsharp_rotate_dims, packed
 
 
-def _free_strides(t: torch.Tensor):
-    """_strides with those of dimensions of size one, which nothing reads, as a dense tensor has them."""
+def _place(t: torch.Tensor):
+    """(t, its strides of batch, head and token), or those of a dense copy where the library cannot be told t's: a tensor
+    broadcast along every dimension (three zeros mean dense there) or along its tokens, rows or a start that are not
+    16-byte aligned, a last dimension with gaps.  Dimensions of size one get a dense tensor's stride: nothing reads it."""
+    b, h, l, e = t.stride()
+    low = _INNER_ONLY[t.dtype]
+    if e == 1 and b and h and l and not (b | h | l) & low and not t.data_ptr() & 15:
+        return t, (b, h, l)
     B, H, L, inner = t.shape
-    dense = (H * L * inner, L * inner, inner)
-    return (C.c_int64 * 3)(*(s if n > 1 else z for s, n, z in zip(t.stride()[:3], (B, H, L), dense)))
+    if B * H * L * inner == 0:
+        return t, (H * L * inner, L * inner, inner)
+    own = (b if B > 1 else H * L * inner, h if H > 1 else L * inner, l if L > 1 else inner)
+    if (e != 1 and inner > 1) or own[2] == 0 or not any(own) or (own[0] | own[1] | own[2]) & low or t.data_ptr() & 15:
+        t = t.clone(memory_format=torch.contiguous_format)
+        return t, t.stride()[:3]
+    return t, own
 
 
 def _check_written(name: str, t: torch.Tensor) -> None:
-    """Refuses an output that holds one place for several values."""
-    if any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
-        raise ValueError(f"{name}: a broadcast tensor cannot be written")
+    """Refuses an output that holds one place for several values or whose last dimension has gaps."""
+    if t.stride(3) != 1 and t.shape[3] > 1 or any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
+        raise ValueError(f"{name}: expected a tensor with a contiguous last dimension and a place for every value")
+
+
+def _written_place(t: torch.Tensor):
+    """An output's strides of batch, head and token; those of dimensions of size one as in a dense tensor."""
+    b, h, l, _ = t.stride()
+    B, H, L, inner = t.shape
+    return (b if B > 1 else H * L * inner, h if H > 1 else L * inner, l if L > 1 else inner)
 
 
 def make_dims(B, H, Lq, Lk, d, dv, M, pool=POOL_PER_BH, q=None, k=None, v=None, y=None,
@@ -383,117 +394,129 @@ class Context:
                                             out.data_ptr()), "fsharp_kernel_apply")
         return out
 
-    def _mine(self, *named):
+    def _mine(self, **named):
         """Refuses tensors that are not on this context's device: the library reads through their pointers unchecked."""
-        for name, t in named:
-            if t is not None and (t.device.type != "cuda" or t.device.index != self.device):
+        for name, t in named.items():
+            if t is not None and t.get_device() != self.device:
                 raise ValueError(f"{name}: expected a tensor on cuda:{self.device}, got {t.device}")
 
     def fsharp_rotate(self, Q, K, rope, pos=None, pos0=0, transpose=False, out=None):
         """Rotary positions (make_rope) on Q [B,H,L,d] and K [B,Hk,L,d] (K may be None): (Q', K').  pos: int64 [B,L] or
         [L], None for 0 .. L-1; pos0 is added to it.  transpose: the gradient.  out: a pair of tensors to write, Q and K
         themselves among them; the default is new dense ones."""
-        self._mine(("Q", Q), ("K", K), ("pos", pos))
-        Q, K = _readable(Q), None if K is None else _readable(K)
+        self._mine(Q=Q, K=K, pos=pos)
+        dt = _dtype_code(Q)
         B, H, L, d = Q.shape
         if K is not None and (K.dim() != 4 or K.shape[0] != B or K.shape[2:] != Q.shape[2:] or K.dtype != Q.dtype):
             raise ValueError(f"K: expected {(B, 'Hk', L, d)} of {Q.dtype}, got {tuple(K.shape)} of {K.dtype}")
-        if pos is not None and (pos.dtype != torch.int64 or tuple(pos.shape) not in ((B, L), (L,))
-                                or (L > 1 and pos.stride(-1) != 1)):
-            raise ValueError("pos: expected int64 [B, L] or [L] whose last dimension is contiguous")
+        pos_stride = 0
+        if pos is not None:
+            if pos.dtype != torch.int64 or tuple(pos.shape) not in ((B, L), (L,)) or (L > 1 and pos.stride(-1) != 1):
+                raise ValueError("pos: expected int64 [B, L] or [L] whose last dimension is contiguous")
+            pos_stride = pos.stride(0) if pos.dim() == 2 else 0
         if out is None:
-            out = (torch.empty(Q.shape, dtype=Q.dtype, device=Q.device),
-                   None if K is None else torch.empty(K.shape, dtype=K.dtype, device=K.device))
-        dm = fsharp_rotate_dims()
-        dm.B, dm.L, dm.H, dm.Hk, dm.d = B, L, H, 0 if K is None else K.shape[1], d
-        for name, x, y in (("q", Q, out[0]), ("k", K, out[1])):
-            if x is not None:
-                self._mine(("out", y))
-                if y.shape != x.shape or y.dtype != x.dtype:
-                    raise ValueError("out: expected the shapes and type of Q and K")
-                _strides(y)
-                _check_written("out", y)
-                setattr(dm, name + "_stride", _free_strides(x))
-                setattr(dm, name + "o_stride", _free_strides(y))
-        _check(self.lib.fsharp_rotate(self._h, Q.data_ptr(), None if K is None else K.data_ptr(),
-                                      None if pos is None else pos.data_ptr(), pos.stride(0) if pos is not None and pos.dim() == 2 else 0,
-                                      pos0, C.byref(rope), C.byref(dm), _dtype_code(Q), int(bool(transpose)), out[0].data_ptr(),
-                                      None if K is None else out[1].data_ptr()), "fsharp_rotate")
-        return out
+            Qo = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+            Ko = None if K is None else torch.empty(K.shape, dtype=K.dtype, device=K.device)
+        else:
+            Qo, Ko = out
+            self._mine(out=Qo, out_k=Ko)
+            for x, y in ((Q, Qo), (K, Ko)):
+                if x is not None:
+                    if y is None or y.shape != x.shape or y.dtype != x.dtype:
+                        raise ValueError("out: expected the shapes and type of Q and K")
+                    _check_written("out", y)
+        Q, sq = _place(Q)
+        so = _written_place(Qo)
+        qp, kp, yp, zp = Q.data_ptr(), None, Qo.data_ptr(), None
+        Hk, sk, sz = 0, (0, 0, 0), (0, 0, 0)
+        if K is not None:
+            K, sk = _place(K)
+            sz = _written_place(Ko)
+            Hk, kp, zp = K.shape[1], K.data_ptr(), Ko.data_ptr()
+        rc = self.lib.fsharp_rotate(self._h, qp, kp, None if pos is None else pos.data_ptr(), pos_stride, pos0, rope,
+                                    _ROTATE_DIMS.pack(B, L, H, Hk, d, *sq, *sk, *so, *sz), dt, 1 if transpose else 0, yp, zp)
+        if rc:
+            raise FsharpError(rc, "fsharp_rotate")
+        return Qo, Ko
 
-    def _cross(self, Q, K, V, scale, key_len, key_mask):
-        """(dims, scale, key_len pointer, key_mask) of a cross attention, its tensors checked."""
+    @staticmethod
+    def _cross_check(Q, K, V, key_len, key_mask):
+        """The sizes (B, H, Hk, Lq, Lk, d, dv) and the mask's stride of a cross attention, its tensors checked."""
         B, H, Lq, d = Q.shape
         if K.dim() != 4 or V.dim() != 4 or K.shape[0] != B or K.shape[3] != d or V.shape[:3] != K.shape[:3] \
                 or K.dtype != Q.dtype or V.dtype != Q.dtype:
             raise ValueError(f"Q {tuple(Q.shape)} {Q.dtype}, K {tuple(K.shape)} {K.dtype}, V {tuple(V.shape)} {V.dtype}: expected "
                              "[B,H,Lq,d], [B,Hk,Lk,d], [B,Hk,Lk,dv] of one type")
-        Hk, Lk = K.shape[1], K.shape[2]
+        _, Hk, Lk, dv = V.shape
         if key_len is not None and (key_len.dtype != torch.int32 or tuple(key_len.shape) != (B,) or not key_len.is_contiguous()):
             raise ValueError("key_len: expected a contiguous int32 [B] tensor")
+        mask_stride = 0
         if key_mask is not None:
             if key_mask.dtype not in (torch.bool, torch.uint8) or tuple(key_mask.shape) not in ((B, Lk), (Lk,)) \
                     or (Lk > 1 and key_mask.stride(-1) != 1):
                 raise ValueError("key_mask: expected bool or uint8 [B, Lk] or [Lk] whose last dimension is contiguous")
-        dm = fsharp_cross_dims()
-        dm.B, dm.H, dm.Hk, dm.Lq, dm.Lk, dm.d, dm.dv = B, H, Hk, Lq, Lk, d, V.shape[3]
-        dm.q_stride, dm.k_stride, dm.v_stride = _free_strides(Q), _free_strides(K), _free_strides(V)
-        dm.mask_stride = key_mask.stride(0) if key_mask is not None and key_mask.dim() == 2 else 0
-        return (dm, d ** -0.5 if scale is None else scale, None if key_len is None else key_len.data_ptr(),
-                None if key_mask is None else key_mask.data_ptr())
+            mask_stride = key_mask.stride(0) if key_mask.dim() == 2 else 0
+        return (B, H, Hk, Lq, Lk, d, dv), mask_stride
 
-    def _cross_scratch(self, dm, dtype, backward, device):
+    def _cross_scratch(self, dims, dtype, backward, device):
         """The call's scratch: a tensor of its own each time, so that the allocator orders its reuse on the stream and a
         captured graph keeps it in its pool."""
-        n = self.lib.fsharp_cross_scratch_bytes(self._h, C.byref(dm), dtype, backward)
-        _check(min(n, 0), "fsharp_cross_scratch_bytes")
-        return (torch.empty(n, dtype=torch.uint8, device=device) if n else None), n
+        n = self.lib.fsharp_cross_scratch_bytes(self._h, dims, dtype, backward)
+        if n <= 0:
+            _check(n, "fsharp_cross_scratch_bytes")
+            return None, None, 0
+        t = torch.empty(n, dtype=torch.uint8, device=device)
+        return t, t.data_ptr(), n
 
     def fsharp_cross_attend(self, Q, K, V, scale=None, key_len=None, key_mask=None, want_lse=False, out=None):
         """Exact softmax attention of Q [B,H,Lq,d] to K [B,Hk,Lk,d], V [B,Hk,Lk,dv]: Y, or (Y, lse [B,H,Lq] float32) with
         want_lse.  scale: d^-1/2 if None.  key_len: int32 [B].  key_mask: bool or uint8 [B,Lk] or [Lk], true where a key
         is seen."""
-        self._mine(("Q", Q), ("K", K), ("V", V), ("key_len", key_len), ("key_mask", key_mask), ("out", out))
-        Q, K, V = _readable(Q), _readable(K), _readable(V)
+        self._mine(Q=Q, K=K, V=V, key_len=key_len, key_mask=key_mask, out=out)
         dt = _dtype_code(Q)
-        dm, scale, lens, mask = self._cross(Q, K, V, scale, key_len, key_mask)
-        B, H, Lq, dv = dm.B, dm.H, dm.Lq, dm.dv
+        sizes, mask_stride = self._cross_check(Q, K, V, key_len, key_mask)
+        B, H, _, Lq, _, d, dv = sizes
+        device = Q.device
         if out is None:
-            out = torch.empty(B, H, Lq, dv, dtype=Q.dtype, device=Q.device)
+            out = torch.empty((B, H, Lq, dv), dtype=Q.dtype, device=device)
         else:
             if tuple(out.shape) != (B, H, Lq, dv) or out.dtype != Q.dtype:
                 raise ValueError(f"out: expected {(B, H, Lq, dv)} of {Q.dtype}")
-            _strides(out)
             _check_written("out", out)
-        dm.y_stride = _free_strides(out)
-        lse = torch.empty(B, H, Lq, dtype=torch.float32, device=Q.device) if want_lse else None
-        scratch, n = self._cross_scratch(dm, dt, 0, Q.device)
-        _check(self.lib.fsharp_cross_attend(self._h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), lens, mask, C.byref(dm), dt, scale,
-                                            out.data_ptr(), lse.data_ptr() if want_lse else None,
-                                            scratch.data_ptr() if n else None, n), "fsharp_cross_attend")
+        (Q, sq), (K, sk), (V, sv) = _place(Q), _place(K), _place(V)
+        lse = torch.empty((B, H, Lq), dtype=torch.float32, device=device) if want_lse else None
+        dims = _CROSS_DIMS.pack(*sizes, *sq, *sk, *sv, *_written_place(out), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, mask_stride)
+        scratch, at, n = self._cross_scratch(dims, dt, 0, device)
+        rc = self.lib.fsharp_cross_attend(self._h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), None if key_len is None else key_len.data_ptr(),
+                                          None if key_mask is None else key_mask.data_ptr(), dims, dt, d ** -0.5 if scale is None else scale,
+                                          out.data_ptr(), lse.data_ptr() if want_lse else None, at, n)
+        if rc:
+            raise FsharpError(rc, "fsharp_cross_attend")
         return (out, lse) if want_lse else out
 
     def fsharp_cross_attend_backward(self, Q, K, V, Y, lse, dY, scale=None, key_len=None, key_mask=None):
         """(dQ, dK, dV) for the cotangent dY of fsharp_cross_attend's Y, with the Y and lse of that call; each gradient is a
-        new tensor with its tensor's shape and, where those are strides of places of its own, strides."""
-        self._mine(("Q", Q), ("K", K), ("V", V), ("Y", Y), ("lse", lse), ("dY", dY), ("key_len", key_len), ("key_mask", key_mask))
-        Q, K, V, Y, dY = (_readable(t) for t in (Q, K, V, Y, dY))
+        new tensor with its tensor's shape and, where those give every value a place of its own, its order of dimensions."""
+        self._mine(Q=Q, K=K, V=V, Y=Y, lse=lse, dY=dY, key_len=key_len, key_mask=key_mask)
         dt = _dtype_code(Q)
-        dm, scale, lens, mask = self._cross(Q, K, V, scale, key_len, key_mask)
-        rows = (dm.B, dm.H, dm.Lq)
+        sizes, mask_stride = self._cross_check(Q, K, V, key_len, key_mask)
+        B, H, _, Lq, _, d, dv = sizes
         for name, t in (("Y", Y), ("dY", dY)):
-            if tuple(t.shape) != rows + (dm.dv,) or t.dtype != Q.dtype:
-                raise ValueError(f"{name}: expected {rows + (dm.dv,)} of {Q.dtype}")
-        if tuple(lse.shape) != rows or lse.dtype != torch.float32 or not lse.is_contiguous():
-            raise ValueError(f"lse: expected a contiguous float32 tensor of shape {rows}")
-        dQ, dK, dV = (torch.empty_like(t) for t in (Q, K, V))      # (the strides of dense and permuted tensors, else dense)
-        dm.y_stride, dm.dy_stride = _free_strides(Y), _free_strides(dY)
-        dm.dq_stride, dm.dk_stride, dm.dv_stride = _free_strides(dQ), _free_strides(dK), _free_strides(dV)
-        scratch, n = self._cross_scratch(dm, dt, 1, Q.device)
-        _check(self.lib.fsharp_cross_attend_backward(
-            self._h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), Y.data_ptr(), lse.data_ptr(), dY.data_ptr(), lens, mask, C.byref(dm),
-            dt, scale, dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), scratch.data_ptr() if n else None, n),
-            "fsharp_cross_attend_backward")
+            if tuple(t.shape) != (B, H, Lq, dv) or t.dtype != Q.dtype:
+                raise ValueError(f"{name}: expected {(B, H, Lq, dv)} of {Q.dtype}")
+        if tuple(lse.shape) != (B, H, Lq) or lse.dtype != torch.float32 or not lse.is_contiguous():
+            raise ValueError(f"lse: expected a contiguous float32 tensor of shape {(B, H, Lq)}")
+        dQ, dK, dV = torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V)      # (permuted like a dense tensor, else dense)
+        (Q, sq), (K, sk), (V, sv), (Y, sy), (dY, sg) = _place(Q), _place(K), _place(V), _place(Y), _place(dY)
+        dims = _CROSS_DIMS.pack(*sizes, *sq, *sk, *sv, *sy, *sg, *_written_place(dQ), *_written_place(dK), *_written_place(dV),
+                                mask_stride)
+        scratch, at, n = self._cross_scratch(dims, dt, 1, Q.device)
+        rc = self.lib.fsharp_cross_attend_backward(
+            self._h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), Y.data_ptr(), lse.data_ptr(), dY.data_ptr(),
+            None if key_len is None else key_len.data_ptr(), None if key_mask is None else key_mask.data_ptr(), dims, dt,
+            d ** -0.5 if scale is None else scale, dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), at, n)
+        if rc:
+            raise FsharpError(rc, "fsharp_cross_attend_backward")
         return dQ, dK, dV
 
     def fsharp_forward_host(self, Q, K, V, Omega, variant, causal=False, chunk=0, pool=POOL_PER_BH,

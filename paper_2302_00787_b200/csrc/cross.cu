@@ -113,6 +113,7 @@ enum Kind { ROWS, FMA, TC };
 struct Plan {
   Kind kind;
   int pieces;
+  bool join;                   // the pieces meet in scratch
   int64_t o_floats, ml;        // partial results
 };
 
@@ -120,11 +121,13 @@ Plan plan_forward(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype)
   Plan p = {};
   const int64_t R = (int64_t)dm->H / dm->Hk * dm->Lq, units = (int64_t)dm->B * dm->Hk;
   if (ctx->impl == FSHARP_IMPL_TENSOR) p.kind = TC;
-  else if (R < FSHARP_CROSS_FEW_ROWS) p.kind = ROWS;
+  else if (R <= fs_cross_rows_most(dtype)) p.kind = ROWS;
   else p.kind = dtype == FSHARP_BF16 && ctx->impl == FSHARP_IMPL_AUTO ? TC : FMA;
   if (dm->Lk == 0) p.kind = FMA;       // (zeros: there is no key that a tensor map could describe)
-  p.pieces = p.kind == ROWS ? fs_cross_rows_pieces(ctx, dm, dtype) : p.kind == TC ? fs_tc_cross_pieces(ctx, dm) : fs_cross_fma_pieces(ctx, dm);
-  if (p.pieces > 1) {
+  bool cluster = false;
+  p.pieces = p.kind == ROWS ? fs_cross_rows_pieces(ctx, dm, dtype, &cluster) : p.kind == TC ? fs_tc_cross_pieces(ctx, dm) : fs_cross_fma_pieces(ctx, dm);
+  p.join = p.pieces > 1 && !cluster;
+  if (p.join) {
     p.ml = units * p.pieces * R;
     p.o_floats = p.ml * dm->dv;
   }
@@ -160,7 +163,7 @@ CrossArgs args_of(const fsharp_cross_dims* dm, const void* Q, const void* K, con
   return a;
 }
 
-int64_t forward_bytes(const Plan& p) { return p.pieces > 1 ? (int64_t)(ws_round(p.o_floats * 4) + ws_round(p.ml * 8)) : 0; }
+int64_t forward_bytes(const Plan& p) { return p.join ? (int64_t)(ws_round(p.o_floats * 4) + ws_round(p.ml * 8)) : 0; }
 int64_t backward_bytes(const GradPlan& p) { return (int64_t)(ws_round(p.stat * 4) + ws_round(p.kv_floats * 4) + ws_round(p.q_floats * 4)); }
 
 int check_scratch(const void* scratch, int64_t have, int64_t need) {
@@ -201,7 +204,7 @@ int fsharp_cross_attend(fsharp_ctx* ctx, const void* Q, const void* K, const voi
   const CrossArgs a = args_of(dims, Q, K, V, key_len, key_mask, scale);
   const TensorAddr ay = fs_addr(dims->y_stride, dims->H, dims->Lq, dims->dv);
   CrossPart part = {nullptr, nullptr, p.pieces};
-  if (p.pieces > 1) {
+  if (p.join) {
     WsAlloc ws{static_cast<char*>(scratch), 0};
     part.o = ws.take<float>(p.o_floats);
     part.ml = ws.take<float2>(p.ml);
@@ -209,7 +212,7 @@ int fsharp_cross_attend(fsharp_ctx* ctx, const void* Q, const void* K, const voi
   if (p.kind == ROWS) FS_TRY(fs_cross_rows(ctx, a, dtype, Y, ay, lse, part));
   else if (p.kind == TC) FS_TRY(fs_tc_cross(ctx, a, Y, ay, lse, part));
   else FS_TRY(fs_cross_fma(ctx, a, dtype, Y, ay, lse, part));
-  return p.pieces > 1 ? fs_cross_join(ctx, a, dtype, Y, ay, lse, part) : FSHARP_OK;
+  return p.join ? fs_cross_join(ctx, a, dtype, Y, ay, lse, part) : FSHARP_OK;
 }
 
 int fsharp_cross_attend_backward(fsharp_ctx* ctx, const void* Q, const void* K, const void* V, const void* Y, const float* lse,

@@ -26,7 +26,7 @@ __device__ __forceinline__ bool cross_seen(const CrossArgs& a, int b, int j, int
 // Pieces of a unit's keys (or rows) that blocks of their own take, so that few units fill the GPU: partial results go to scratch.
 // Forward: O [unit][piece][R][dv] (unnormalised) and (m, l) [unit][piece][R].
 struct CrossPart {
-  float* o;
+  float* o;              // null where there is one piece, or where a unit's pieces meet in a cluster
   float2* ml;
   int pieces;
 };
@@ -38,7 +38,8 @@ int fs_tc_cross_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm);
 int fs_tc_cross(fsharp_ctx* ctx, const CrossArgs& a, void* Y, TensorAddr ay, float* lse, CrossPart part);
 
 // few rows (cross_rows.cu), and the join of pieces
-int fs_cross_rows_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype);
+int fs_cross_rows_most(int dtype);
+int fs_cross_rows_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype, bool* cluster);
 int fs_cross_rows(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, TensorAddr ay, float* lse, CrossPart part);
 int fs_cross_join(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, TensorAddr ay, float* lse, CrossPart part);
 // multiply-add tiles (cross_fma.cu)

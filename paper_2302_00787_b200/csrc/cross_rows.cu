@@ -1,16 +1,22 @@
-// Cross attention of few query rows per key head (decoding steps): K and V are streamed once, straight from memory into
-// registers.  A key's d values lie across D / VE lanes (16 bytes each), a warp's load covers 512 bytes of K or V, and the
-// loads of four keys per lane and of their values are in flight together; scores are sums over a key's lanes by shuffles.
-// Each lane group keeps a maximum, a sum and an output of its own; they meet once at the end (warp, block, then the
-// pieces by cross_join_kernel).
-// Bound: HBM (2 n d bytes per element size and unit).
+// Cross attention of few query rows per key head (decoding steps): K and V are streamed once.  A key's d values lie across
+// D / VE lanes (16 bytes each), a warp's copy covers 512 bytes of K or V, and asynchronous copies of up to three turns of four keys
+// and values per lane are in flight (up to 190 KB per SM); scores are sums over a key's lanes by shuffles.
+// Each lane group keeps a maximum, a sum and an output of its own; they meet once at the end: warp, block, then the pieces of
+// the keys, which are the blocks of a cluster (up to eight; one launch) or meet in scratch (cross_join_kernel).
+// Bound: HBM (2 n d values per unit).
 #include "cross.cuh"
 #include "tc_common.cuh"
 
 namespace {
 
-constexpr int RW_T = 256, RW_WARPS = RW_T / 32, RW_U = 4;
+constexpr int RW_T = 128, RW_WARPS = RW_T / 32, RW_U = 4, RW_STAGES = 3;
+constexpr size_t RW_RING = (size_t)RW_STAGES * 2 * RW_U * RW_T * 16;      // 48 KB: four blocks on an SM
+constexpr int RW_CLUSTER = 8;      // most pieces that meet in a cluster
 
+// 16 bytes into shared memory behind the registers' back, zeros where there is nothing to read
+__device__ __forceinline__ void copy16(uint4* to, const void* from, bool some) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(to)), "l"(from), "r"(some ? 16 : 0) : "memory");
+}
 template <typename T> __device__ __forceinline__ void widen(const uint4& x, float* v);
 template <> __device__ __forceinline__ void widen<float>(const uint4& x, float* v) {
   v[0] = __uint_as_float(x.x); v[1] = __uint_as_float(x.y); v[2] = __uint_as_float(x.z); v[3] = __uint_as_float(x.w);
@@ -56,22 +62,43 @@ cross_rows_kernel(const __grid_constant__ CrossArgs a, T* __restrict__ Y, Tensor
 #pragma unroll
     for (int k = 0; k < VE; k++) o[r][k] = 0.f;
   }
-  for (int t = t0; t < t1; t++) {
-    uint4 kx[RW_U], vx[RW_U];
-    bool seen[RW_U];
+  // A thread's ring in shared memory, RW_STAGES turns of its own 16-byte pieces: nobody else touches them, so waiting for the thread's
+  // own copies is all the order they need.
+  extern __shared__ uint4 ring[];
+  uint4* mine = ring + threadIdx.x;
+  auto fetch = [&](int t) {
+    if (t < t1) {
+      uint4* to = mine + (t % RW_STAGES) * 2 * RW_U * RW_T;
 #pragma unroll
-    for (int u = 0; u < RW_U; u++) {
-      const int j = t * STEP + (u * RW_WARPS + warp) * KPW + grp;
-      kx[u] = vx[u] = make_uint4(0, 0, 0, 0);
-      if (j < n && inq) kx[u] = __ldg(reinterpret_cast<const uint4*>(Kb + j * a.ak.sl));
-      if (j < n && inv) vx[u] = __ldg(reinterpret_cast<const uint4*>(Vb + j * a.av.sl));
-      seen[u] = cross_seen(a, b, j, n);
+      for (int u = 0; u < RW_U; u++) {
+        const int64_t j = t * STEP + (u * RW_WARPS + warp) * KPW + grp;
+        copy16(to + 2 * u * RW_T, Kb + (j < n ? j * a.ak.sl : 0), j < n && inq);
+        copy16(to + (2 * u + 1) * RW_T, Vb + (j < n ? j * a.av.sl : 0), j < n && inv);
+      }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  bool next[RW_U];                                       // which keys of the coming turn are seen
+  auto look = [&](int t) {
+#pragma unroll
+    for (int u = 0; u < RW_U; u++) next[u] = cross_seen(a, b, t * STEP + (u * RW_WARPS + warp) * KPW + grp, n);
+  };
+#pragma unroll
+  for (int t = 0; t < RW_STAGES - 1; t++) fetch(t0 + t);
+  if (t0 < t1) look(t0);
+  for (int t = t0; t < t1; t++) {
+    fetch(t + RW_STAGES - 1);
+    bool on[RW_U];
+#pragma unroll
+    for (int u = 0; u < RW_U; u++) on[u] = next[u];
+    if (t + 1 < t1) look(t + 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(RW_STAGES - 1) : "memory");
+    const uint4* from = mine + (t % RW_STAGES) * 2 * RW_U * RW_T;
     float s[RW_U][R];
 #pragma unroll
     for (int u = 0; u < RW_U; u++) {
       float k[VE];
-      widen<T>(kx[u], k);
+      widen<T>(from[2 * u * RW_T], k);
 #pragma unroll
       for (int r = 0; r < R; r++) {
         float x = 0.f;
@@ -91,7 +118,7 @@ cross_rows_kernel(const __grid_constant__ CrossArgs a, T* __restrict__ Y, Tensor
       float top = m[r];
 #pragma unroll
       for (int u = 0; u < RW_U; u++) {
-        if (!seen[u]) s[u][r] = -INFINITY;
+        if (!on[u]) s[u][r] = -INFINITY;
         top = fmaxf(top, s[u][r]);
       }
       const float base = top == -INFINITY ? 0.f : top, corr = tc::ex2(m[r] - base);
@@ -107,9 +134,10 @@ cross_rows_kernel(const __grid_constant__ CrossArgs a, T* __restrict__ Y, Tensor
     }
 #pragma unroll
     for (int u = 0; u < RW_U; u++) {
-      if (!seen[u]) vx[u] = make_uint4(0, 0, 0, 0);      // what a hidden key holds may be anything
+      uint4 y = from[(2 * u + 1) * RW_T];
+      if (!on[u]) y = make_uint4(0, 0, 0, 0);            // what a hidden key holds may be anything
       float v[VE];
-      widen<T>(vx[u], v);
+      widen<T>(y, v);
 #pragma unroll
       for (int r = 0; r < R; r++)
 #pragma unroll
@@ -139,30 +167,59 @@ cross_rows_kernel(const __grid_constant__ CrossArgs a, T* __restrict__ Y, Tensor
     }
   }
   __syncthreads();
+  // the block's sums, in the first warp's place
   for (int i = threadIdx.x; i < R * D; i += RW_T) {
     const int r = i / D, e = i % D;
-    if (r >= rows || e >= a.dv) continue;
-    float top = -INFINITY;
+    float top = sm[0][r], x = 0.f;
 #pragma unroll
-    for (int w = 0; w < RW_WARPS; w++) top = fmaxf(top, sm[w][r]);
+    for (int w = 1; w < RW_WARPS; w++) top = fmaxf(top, sm[w][r]);
     const float base = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, x = 0.f;
 #pragma unroll
-    for (int w = 0; w < RW_WARPS; w++) {
-      const float f = tc::ex2(sm[w][r] - base);
-      sum = fmaf(f, sl[w][r], sum);
-      x = fmaf(f, so[w][r][e], x);
-    }
-    if (part.pieces > 1) {
-      const int64_t at = ((int64_t)unit * part.pieces + piece) * rows + r;
-      part.o[at * a.dv + e] = x;
-      if (e == 0) part.ml[at] = make_float2(top, sum);
-    } else {
-      const int h = hk * a.g + r / a.Lq, tok = r % a.Lq;
-      fs_store(Y + b * ay.sb + h * ay.sh + tok * ay.sl + e, sum == 0.f ? 0.f : x / sum);
-      if (lse && e == 0) lse[((int64_t)b * a.H + h) * a.Lq + tok] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * FS_LN2;
-    }
+    for (int w = 0; w < RW_WARPS; w++) x = fmaf(tc::ex2(sm[w][r] - base), so[w][r][e], x);
+    so[0][r][e] = x;
   }
+  __syncthreads();
+  if (threadIdx.x < R) {
+    const int r = threadIdx.x;
+    float top = sm[0][r], sum = 0.f;
+#pragma unroll
+    for (int w = 1; w < RW_WARPS; w++) top = fmaxf(top, sm[w][r]);
+    const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int w = 0; w < RW_WARPS; w++) sum = fmaf(tc::ex2(sm[w][r] - base), sl[w][r], sum);
+    sm[0][r] = top;
+    sl[0][r] = sum;
+  }
+  const bool cluster = !part.o && part.pieces > 1;
+  if (cluster) tc::cluster_sync();
+  else __syncthreads();
+  if (!cluster || piece == 0)
+    for (int i = threadIdx.x; i < R * D; i += RW_T) {
+      const int r = i / D, e = i % D;
+      if (r >= rows || e >= a.dv) continue;
+      float top = sm[0][r], sum = sl[0][r], x = so[0][r][e];
+      if (cluster) {
+        const uint32_t am = tc::smem_u32(&sm[0][r]), al = tc::smem_u32(&sl[0][r]), ao = tc::smem_u32(&so[0][r][e]);
+        for (int p = 1; p < part.pieces; p++) top = fmaxf(top, tc::load_cluster(tc::map_cluster(am, p)));
+        const float base = top == -INFINITY ? 0.f : top;
+        sum = x = 0.f;
+        for (int p = 0; p < part.pieces; p++) {
+          const float f = tc::ex2(tc::load_cluster(tc::map_cluster(am, p)) - base);
+          sum = fmaf(f, tc::load_cluster(tc::map_cluster(al, p)), sum);
+          x = fmaf(f, tc::load_cluster(tc::map_cluster(ao, p)), x);
+        }
+      }
+      if (part.o) {
+        const int64_t at = ((int64_t)unit * part.pieces + piece) * rows + r;
+        part.o[at * a.dv + e] = x;
+        if (e == 0) part.ml[at] = make_float2(top, sum);
+      } else {
+        const int h = hk * a.g + r / a.Lq, tok = r % a.Lq;
+        fs_store(Y + b * ay.sb + h * ay.sh + tok * ay.sl + e, sum == 0.f ? 0.f : x / sum);
+        if (lse && e == 0) lse[((int64_t)b * a.H + h) * a.Lq + tok] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * FS_LN2;
+      }
+    }
+  if (cluster) tc::cluster_sync();      // (a block's shared memory is read until here)
 }
 
 // Y and lse from the pieces' partial results: a thread per row and four values.
@@ -198,26 +255,37 @@ cross_join_kernel(CrossPart part, int64_t units, int Hk, int R, int g, int Lq, i
   if (lse && e == 0) lse[(b * Hk * g + h) * Lq + tok] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * FS_LN2;
 }
 
-template <typename T, int D>
-void launch_rows(fsharp_ctx* ctx, const CrossArgs& a, T* Y, TensorAddr ay, float* lse, CrossPart part) {
-  const dim3 grid((unsigned)part.pieces, (unsigned)(a.B * a.Hk));
-  const int R = a.g * a.Lq;
-  if (R == 1) cross_rows_kernel<T, D, 1><<<grid, RW_T, 0, ctx->stream>>>(a, Y, ay, lse, part);
-  else if (R == 2) cross_rows_kernel<T, D, 2><<<grid, RW_T, 0, ctx->stream>>>(a, Y, ay, lse, part);
-  else cross_rows_kernel<T, D, 4><<<grid, RW_T, 0, ctx->stream>>>(a, Y, ay, lse, part);
-}
-
-template <typename T>
-int run_rows(fsharp_ctx* ctx, const CrossArgs& a, T* Y, TensorAddr ay, float* lse, CrossPart part) {
-  const int D = a.d > a.dv ? a.d : a.dv;
+template <typename T, int D, int R>
+int launch_rows(fsharp_ctx* ctx, const CrossArgs& a, T* Y, TensorAddr ay, float* lse, CrossPart part) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)part.pieces, (unsigned)(a.B * a.Hk));
+  cfg.blockDim = dim3(RW_T);
+  cfg.dynamicSmemBytes = RW_RING;
+  cfg.stream = ctx->stream;
+  cudaLaunchAttribute at[1];
+  if (!part.o && part.pieces > 1) {
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)part.pieces;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+  }
+  FS_CUDA_OK(fs_allow_smem(cross_rows_kernel<T, D, R>, sizeof(float) * RW_WARPS * R * (D + 2)));
   FS_TIME_BEGIN(ctx, FS_K_CROSS_ROWS);
-  if (D == 16) launch_rows<T, 16>(ctx, a, Y, ay, lse, part);
-  else if (D == 32) launch_rows<T, 32>(ctx, a, Y, ay, lse, part);
-  else if (D == 64) launch_rows<T, 64>(ctx, a, Y, ay, lse, part);
-  else launch_rows<T, 128>(ctx, a, Y, ay, lse, part);
+  FS_CUDA_OK(cudaLaunchKernelEx(&cfg, cross_rows_kernel<T, D, R>, a, Y, ay, lse, part));
   FS_TIME_END(ctx);
   FS_LAUNCH_CHECK(ctx);
   return FSHARP_OK;
+}
+
+template <typename T, int R>
+int run_rows(fsharp_ctx* ctx, const CrossArgs& a, void* Yv, TensorAddr ay, float* lse, CrossPart part) {
+  const int D = a.d > a.dv ? a.d : a.dv;
+  T* Y = static_cast<T*>(Yv);
+  if (D == 16) return launch_rows<T, 16, R>(ctx, a, Y, ay, lse, part);
+  if (D == 32) return launch_rows<T, 32, R>(ctx, a, Y, ay, lse, part);
+  if (D == 64) return launch_rows<T, 64, R>(ctx, a, Y, ay, lse, part);
+  return launch_rows<T, 128, R>(ctx, a, Y, ay, lse, part);
 }
 
 template <typename T>
@@ -235,19 +303,28 @@ int run_join(fsharp_ctx* ctx, const CrossArgs& a, T* Y, TensorAddr ay, float* ls
 
 }  // namespace
 
-// As many pieces as fill the GPU with four blocks per SM, each with a turn of keys at least.
-int fs_cross_rows_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype) {
+// Up to how many rows of a unit this kernel is the one to take: one of bf16 (more go to the tensor cores, which take up to 128 at the
+// price of one: 16 x 4 key heads, 16384 keys, d = 128: 182 us here and 165 there for one row, 249 and 90 for two), four of fp32.
+int fs_cross_rows_most(int dtype) { return dtype == FSHARP_F32 ? 4 : 1; }
+
+// Pieces of the keys: enough for twelve blocks per SM, which even out sequences of different lengths, each with two turns of keys
+// where eight pieces (a cluster) do; where they leave SMs without work, as many more, through scratch, as give every SM four blocks.
+int fs_cross_rows_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype, bool* cluster) {
   const int es = dtype == FSHARP_F32 ? 4 : 2, D = dm->d > dm->dv ? dm->d : dm->dv, step = rows_step(D, es);
-  const int64_t units = (int64_t)dm->B * dm->Hk, turns = ((int64_t)dm->Lk + step - 1) / step;
-  int64_t p = 4 * (int64_t)ctx->sm_count / units;
-  if (p > turns) p = turns;
-  if (p > 128) p = 128;
-  return p < 1 ? 1 : (int)p;
+  const int64_t units = (int64_t)dm->B * dm->Hk, turns = ((int64_t)dm->Lk + step - 1) / step, sms = ctx->sm_count;
+  int64_t p = (12 * sms + units - 1) / units;
+  if (p > turns / 2) p = turns / 2;
+  *cluster = p <= RW_CLUSTER || units * RW_CLUSTER >= 2 * sms;
+  if (*cluster) p = p > RW_CLUSTER ? RW_CLUSTER : p;
+  else p = p < 4 * sms / units ? p : 4 * sms / units;
+  return p < 1 ? 1 : p > 256 ? 256 : (int)p;
 }
 
 int fs_cross_rows(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, TensorAddr ay, float* lse, CrossPart part) {
-  return dtype == FSHARP_F32 ? run_rows<float>(ctx, a, static_cast<float*>(Y), ay, lse, part)
-                             : run_rows<__nv_bfloat16>(ctx, a, static_cast<__nv_bfloat16*>(Y), ay, lse, part);
+  const int R = a.g * a.Lq;
+  if (dtype == FSHARP_BF16) return run_rows<__nv_bfloat16, 1>(ctx, a, Y, ay, lse, part);
+  return R == 1 ? run_rows<float, 1>(ctx, a, Y, ay, lse, part) : R == 2 ? run_rows<float, 2>(ctx, a, Y, ay, lse, part)
+                                                               : run_rows<float, 4>(ctx, a, Y, ay, lse, part);
 }
 int fs_cross_join(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, TensorAddr ay, float* lse, CrossPart part) {
   return dtype == FSHARP_F32 ? run_join<float>(ctx, a, static_cast<float*>(Y), ay, lse, part)

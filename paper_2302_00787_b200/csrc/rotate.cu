@@ -10,6 +10,7 @@
 #include <math.h>
 
 #include "common.cuh"
+#include "tc_common.cuh"
 
 namespace {
 
@@ -25,15 +26,40 @@ struct RotFreq {
   double turns[64];      // per position
 };
 
+// W neighbouring values of a row, as one load or store; bf16 pairs are widened and rounded two at a time.
 template <typename T, int W>
 struct alignas(sizeof(T) * W) Vec {
   T v[W];
 };
+template <int W> __device__ __forceinline__ void widen(const Vec<float, W>& x, float* f) {
+#pragma unroll
+  for (int k = 0; k < W; k++) f[k] = x.v[k];
+}
+template <int W> __device__ __forceinline__ void widen(const Vec<__nv_bfloat16, W>& x, float* f) {
+  if constexpr (W == 1) f[0] = __bfloat162float(x.v[0]);
+  else {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(x.v);
+#pragma unroll
+    for (int k = 0; k < W; k += 2) { f[k] = __uint_as_float(w[k / 2] << 16); f[k + 1] = __uint_as_float(w[k / 2] & 0xffff0000u); }
+  }
+}
+template <int W> __device__ __forceinline__ void narrow(Vec<float, W>& x, const float* f) {
+#pragma unroll
+  for (int k = 0; k < W; k++) x.v[k] = f[k];
+}
+template <int W> __device__ __forceinline__ void narrow(Vec<__nv_bfloat16, W>& x, const float* f) {
+  if constexpr (W == 1) x.v[0] = __float2bfloat16_rn(f[0]);
+  else {
+    uint32_t* w = reinterpret_cast<uint32_t*>(x.v);
+#pragma unroll
+    for (int k = 0; k < W; k += 2) w[k / 2] = tc::pack_bf16(f[k], f[k + 1]);
+  }
+}
 
-template <typename T, int W>
+template <typename T, int W, bool INTERLEAVED>
 __global__ void __launch_bounds__(ROT_T)
-rotate_kernel(RotTensors t, const __grid_constant__ RotFreq freq, const int64_t* __restrict__ pos, int64_t pos_stride, int64_t pos0,
-              int64_t tokens, int L, int d, int rot, int interleaved, int hpt, float gain, float sign) {
+rotate_kernel(const __grid_constant__ RotTensors t, const __grid_constant__ RotFreq freq, const int64_t* __restrict__ pos, int64_t pos_stride,
+              int64_t pos0, int64_t tokens, int L, int d, int rot, int hpt, float gain, float sign) {
   const int units = d / (2 * W);                      // a power of two
   const int64_t g = (int64_t)blockIdx.x * ROT_T + threadIdx.x;
   const int64_t tok = g / units;
@@ -43,72 +69,58 @@ rotate_kernel(RotTensors t, const __grid_constant__ RotFreq freq, const int64_t*
   // pairs u W .. u W + W - 1; those past rot / 2 (a multiple of W) are neighbours that pass through
   const int p0 = u * W;
   const bool turn = p0 < rot / 2;
-  int ja, jb;
-  if (interleaved) { ja = 2 * p0; jb = ja + W; }
-  else if (turn) { ja = p0; jb = p0 + rot / 2; }
-  else { ja = 2 * p0; jb = ja + W; }                  // = rot + 2 (p0 - rot / 2)
+  const int ja = turn && !INTERLEAVED ? p0 : 2 * p0, jb = turn && !INTERLEAVED ? p0 + rot / 2 : 2 * p0 + W;
   float c[W], s[W];
+#pragma unroll
+  for (int k = 0; k < W; k++) { c[k] = 1.f; s[k] = 0.f; }
   if (turn) {
     const double p = (double)((pos ? pos[b * pos_stride + i] : i) + pos0);
 #pragma unroll
     for (int k = 0; k < W; k++) {
       const double n = p * freq.turns[p0 + k];
-      float sn, cs;
-      sincospif(2.f * (float)(n - rint(n)), &sn, &cs);
-      c[k] = gain * cs;
-      s[k] = gain * sign * sn;
+      sincospif(2.f * (float)(n - rint(n)), &s[k], &c[k]);
+      c[k] *= gain;
+      s[k] *= gain * sign;
     }
-  } else {
-#pragma unroll
-    for (int k = 0; k < W; k++) { c[k] = 1.f; s[k] = 0.f; }
   }
-  const int heads = t.H[0] + t.H[1], h0 = blockIdx.y * hpt, h1 = min(heads, h0 + hpt);
   using V = Vec<T, W>;
-  auto at = [&](int h, const T*& x, T*& y) {
-    const int w = h >= t.H[0];
-    const int64_t hh = w ? h - t.H[0] : h;
-    x = static_cast<const T*>(t.x[w]) + b * t.ax[w].sb + hh * t.ax[w].sh + i * t.ax[w].sl;
-    y = static_cast<T*>(t.y[w]) + b * t.ay[w].sb + hh * t.ay[w].sh + i * t.ay[w].sl;
-  };
   constexpr int U = 4;                                // heads with their loads in flight together
-  for (int h = h0; h < h1; h += U) {
-    V a[U], e[U];
-    T* out[U];
+  const int h0 = blockIdx.y * hpt, h1 = h0 + hpt;
 #pragma unroll
-    for (int q = 0; q < U; q++)
-      if (h + q < h1) {
-        const T* x;
-        at(h + q, x, out[q]);
-        a[q] = *reinterpret_cast<const V*>(x + ja);
-        e[q] = *reinterpret_cast<const V*>(x + jb);
-      }
+  for (int w = 0; w < 2; w++) {
+    const int first = w ? max(0, h0 - t.H[0]) : h0, last = w ? min(t.H[1], h1 - t.H[0]) : min(t.H[0], h1);
+    if (first >= last) continue;
+    const int64_t sx = t.ax[w].sh, sy = t.ay[w].sh;
+    const T* x = static_cast<const T*>(t.x[w]) + b * t.ax[w].sb + i * t.ax[w].sl + first * sx;
+    T* y = static_cast<T*>(t.y[w]) + b * t.ay[w].sb + i * t.ay[w].sl + first * sy;
+    for (int h = first; h < last; h += U, x += U * sx, y += U * sy) {
+      V a[U], e[U];
 #pragma unroll
-    for (int q = 0; q < U; q++)
-      if (h + q < h1) {
-        V ya, yb;
-        if (interleaved && W > 1) {
-          // the unit's 2 W values in a row: pair k is (2k, 2k + 1)
-          float z[2 * W];
-#pragma unroll
-          for (int k = 0; k < W; k++) { z[k] = fs_load(&a[q].v[k]); z[W + k] = fs_load(&e[q].v[k]); }
-#pragma unroll
-          for (int k = 0; k < W; k++) {
-            const float r = z[2 * k] * c[k] - z[2 * k + 1] * s[k], m = z[2 * k + 1] * c[k] + z[2 * k] * s[k];
-            fs_store(2 * k < W ? &ya.v[(2 * k) % W] : &yb.v[(2 * k) % W], r);
-            fs_store(2 * k + 1 < W ? &ya.v[(2 * k + 1) % W] : &yb.v[(2 * k + 1) % W], m);
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < W; k++) {
-            const float x0 = fs_load(&a[q].v[k]), x1 = fs_load(&e[q].v[k]);
-            fs_store(&ya.v[k], x0 * c[k] - x1 * s[k]);
-            fs_store(&yb.v[k], x1 * c[k] + x0 * s[k]);
-          }
+      for (int q = 0; q < U; q++)
+        if (h + q < last) {
+          a[q] = *reinterpret_cast<const V*>(x + q * sx + ja);
+          e[q] = *reinterpret_cast<const V*>(x + q * sx + jb);
         }
-        if (!turn) { ya = a[q]; yb = e[q]; }          // the bits as they are, NaNs among them
-        *reinterpret_cast<V*>(out[q] + ja) = ya;
-        *reinterpret_cast<V*>(out[q] + jb) = yb;
-      }
+#pragma unroll
+      for (int q = 0; q < U; q++)
+        if (h + q < last) {
+          if (turn) {                                 // (what passes through keeps its bits, NaNs among them)
+            float z[2 * W], r[2 * W];
+            widen<W>(a[q], z);
+            widen<W>(e[q], z + W);
+#pragma unroll
+            for (int k = 0; k < W; k++) {
+              const int m = INTERLEAVED ? 2 * k : k, n = INTERLEAVED ? 2 * k + 1 : W + k;
+              r[m] = z[m] * c[k] - z[n] * s[k];
+              r[n] = z[n] * c[k] + z[m] * s[k];
+            }
+            narrow<W>(a[q], r);
+            narrow<W>(e[q], r + W);
+          }
+          *reinterpret_cast<V*>(y + q * sy + ja) = a[q];
+          *reinterpret_cast<V*>(y + q * sy + jb) = e[q];
+        }
+    }
   }
 }
 
@@ -117,15 +129,15 @@ int launch(fsharp_ctx* ctx, const RotTensors& t, const RotFreq& f, const int64_t
            int L, int d, const fsharp_rope* r, int transpose) {
   const int heads = t.H[0] + t.H[1];
   const int64_t units = tokens * (d / (2 * W));
-  // Heads per thread: as many as leave the GPU full (the angles are shared by them), at most 8.
-  int64_t hpt = units * heads / ((int64_t)ctx->sm_count * 2048);
-  hpt = hpt < 1 ? 1 : hpt > 8 ? 8 : hpt;
+  // Heads per thread: as many as leave a thousand threads per SM (the angles are shared by them).
+  int64_t hpt = units * heads / ((int64_t)ctx->sm_count * 1024);
+  hpt = hpt < 1 ? 1 : hpt > heads ? heads : hpt;
   const int64_t gx = (units + ROT_T - 1) / ROT_T, gy = (heads + hpt - 1) / hpt;
   if (gx > 0x7fffffff || gy > 65535) return FSHARP_E_SHAPE;
   FS_TIME_BEGIN(ctx, FS_K_ROTATE);
-  rotate_kernel<T, W><<<dim3((unsigned)gx, (unsigned)gy), ROT_T, 0, ctx->stream>>>(
-      t, f, pos, pos_stride, pos0, tokens, L, d, r->rot, r->layout == FSHARP_ROT_INTERLEAVED, (int)hpt, (float)r->gain,
-      transpose ? -1.f : 1.f);
+  const auto kernel = r->layout == FSHARP_ROT_INTERLEAVED ? rotate_kernel<T, W, true> : rotate_kernel<T, W, false>;
+  kernel<<<dim3((unsigned)gx, (unsigned)gy), ROT_T, 0, ctx->stream>>>(t, f, pos, pos_stride, pos0, tokens, L, d, r->rot, (int)hpt,
+                                                                      (float)r->gain, transpose ? -1.f : 1.f);
   FS_TIME_END(ctx);
   FS_LAUNCH_CHECK(ctx);
   return FSHARP_OK;

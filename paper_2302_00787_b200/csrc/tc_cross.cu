@@ -1,7 +1,7 @@
 // Exact cross attention of bf16 tensors on the tensor cores:  Y = softmax(scale Q K^T) V  with a running maximum.
 //
 // A block has up to 256 rows of a unit (rows are packed over the query heads that share a key head) and walks the unit's keys
-// in tiles of 128.  Two warpgroups, thread = row: each has scores S (128 lanes x 128 columns of tensor memory), from which its
+// in tiles of 128.  Two warpgroups, thread = row: each has scores S (lanes: rows, columns: keys of tensor memory), from which its
 // threads read a row, take the maximum and the exponentials and put them back as bf16 P over S, and an output O that the
 // tensor core adds P V to from there.  Warps of their own copy K and V tiles (TMA, one ring, K before V) and issue the
 // products: S of the next tile and P V of one warpgroup run while the other one is at its exponentials.
@@ -23,18 +23,29 @@ using namespace tcx;
 namespace {
 
 constexpr int CX_WARPS = 8, CXW_TMA = 8, CXW_MMA = 9, CX_T = 384;      // (warps 10, 11 only hand their registers over)
-constexpr uint32_t CX_TMEM = 512, CX_S = 0, CX_O = 256;      // S of the two warpgroups, then O (128 columns apart)
+constexpr int CX_REGS_REST = 56, CX_REGS_ROWS = 224;                   // 384 threads x 168 at launch = 128 x 56 + 256 x 224
+constexpr uint32_t CX_TMEM = 512;
 constexpr float CX_SLACK = 8.f;
+#ifndef CX_CUBIC
+#define CX_CUBIC 3
+#endif
 
 template <int D>
 struct CxSm {
-  static constexpr int PANELS = D / 64, NS = D == 64 ? 8 : 5;      // slots of the ring: a K or V tile each
-  static constexpr uint32_t SLOT = PANELS * TILE_BYTES, Q = 0, RING = 2 * SLOT, MISC = RING + NS * SLOT, TOTAL = MISC + 512;
+  static constexpr int PANELS = D / 64, KT = 128, NS = D == 64 ? 8 : 5;      // keys per tile; slots of the ring: a K or V tile each
+  static constexpr uint32_t PANEL = KT * 128, SLOT = PANELS * PANEL, QT = PANELS * TILE_BYTES, Q = 0, RING = 2 * QT;
+  static constexpr uint32_t MISC = RING + NS * SLOT, TOTAL = MISC + 512;
+  // Columns of a warpgroup: S, P (two to a column), O.  At d = 64 P has a place of its own and S is free for the next tile as soon as
+  // it has been read; d = 128 has no room for that, there P lies over S.  (Tiles of 64 keys would make room; their S, N = 64, is
+  // bound by shared memory: 16 heads on 4, 2049 x 10007, 285 us instead of 228.)
+  static constexpr bool OVER = D == 128;
+  static constexpr uint32_t S = 0, P = OVER ? 0 : KT, O = OVER ? KT : KT + KT / 2, GROUP = 256;
   static_assert(TOTAL + 1024 <= 232448, "shared memory budget");
   static_assert(NS * SLOT >= 128 * (D + 1) * 4 + 1024, "the warpgroups' exchange");
+  static_assert(O + D <= GROUP, "tensor memory");
 };
 struct CxMs {
-  uint64_t full[8], empty[8], s_full[2], p_ready[2], o_full[2], q_ready;
+  uint64_t full[8], empty[8], s_full[2], s_free[2], p_ready[2], o_full[2], q_ready;
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -45,6 +56,7 @@ __global__ void __launch_bounds__(CX_T, 1)
 tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CrossArgs a,
                 __nv_bfloat16* __restrict__ Y, TensorAddr ay, float* __restrict__ lse, CrossPart part, int* __restrict__ status) {
   using Sm = CxSm<D>;
+  constexpr int KT = Sm::KT;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   CxMs* misc = reinterpret_cast<CxMs*>(sm + Sm::MISC);
@@ -52,14 +64,14 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   volatile int* abortp = &misc->abort_flag;
   const int unit = blockIdx.y, piece = blockIdx.x % part.pieces, r0 = (int)(blockIdx.x / part.pieces) * 256;
   const int b = unit / a.Hk, hk = unit % a.Hk, R = a.g * a.Lq;
-  const int n = cross_keys(a, b), tiles = (n + TILE - 1) / TILE;
+  const int n = cross_keys(a, b), tiles = (n + KT - 1) / KT;
   const int t0 = (int)((int64_t)tiles * piece / part.pieces), nt = (int)((int64_t)tiles * (piece + 1) / part.pieces) - t0;
   const bool both = R - r0 > TILE;                     // each warpgroup has rows of its own
   const int items = both ? 2 * nt : nt;                // item i: warpgroup i & 1, tile i / 2 or i
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < Sm::NS; i++) { mbar_init(&misc->full[i], 1); mbar_init(&misc->empty[i], 1); }
-    for (int w = 0; w < 2; w++) { mbar_init(&misc->s_full[w], 1); mbar_init(&misc->p_ready[w], 4); mbar_init(&misc->o_full[w], 1); }
+    for (int w = 0; w < 2; w++) { mbar_init(&misc->s_full[w], 1); mbar_init(&misc->s_free[w], 4); mbar_init(&misc->p_ready[w], 4); mbar_init(&misc->o_full[w], 1); }
     mbar_init(&misc->q_ready, CX_WARPS);
     misc->abort_flag = 0;
     fence_barrier_init();
@@ -74,7 +86,7 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   const uint32_t tmem = misc->tmem_base;
   const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;      // panels of 64 columns
 
-  if (warp >= CX_WARPS) regs_release<REGS_PRODUCER>();
+  if (warp >= CX_WARPS) regs_release<CX_REGS_REST>();
   if (warp == CXW_TMA) {
     if (lane == 0) {
       prefetch_tmap(&tmK); prefetch_tmap(&tmV);
@@ -83,64 +95,73 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       // (a stride of zero, one entry for all, is a dimension of size one in the tensor map)
       const int ch[2] = {a.ak.sh ? hk : 0, a.av.sh ? hk : 0}, cb[2] = {a.ak.sb ? b : 0, a.av.sb ? b : 0};
       for (; issued < 2 * nt && ok; issued++) {
-        const int s = issued % Sm::NS, tok = (t0 + issued / 2) * TILE;
+        const int s = issued % Sm::NS, tok = (t0 + issued / 2) * KT;
         if (!mbar_wait(&misc->empty[s], ((issued / Sm::NS) & 1) ^ 1, abortp, status)) { ok = false; break; }
         uint8_t* base = sm + Sm::RING + s * Sm::SLOT;
         const CUtensorMap* map = issued & 1 ? &tmV : &tmK;
         const int panels = issued & 1 ? vp : kp;
-        mbar_expect_tx(&misc->full[s], panels * TILE_BYTES);
-        for (int p = 0; p < panels; p++) tma_load_4d(base + p * TILE_BYTES, map, &misc->full[s], p * 64, tok, ch[issued & 1], cb[issued & 1]);
+        mbar_expect_tx(&misc->full[s], panels * Sm::PANEL);
+        for (int p = 0; p < panels; p++) tma_load_4d(base + p * Sm::PANEL, map, &misc->full[s], p * 64, tok, ch[issued & 1], cb[issued & 1]);
       }
-      // no copy of this block may still be in flight when it exits
-      for (int i = max(0, issued - Sm::NS); i < issued; i++) mbar_wait(&misc->full[i % Sm::NS], (i / Sm::NS) & 1, abortp, status, false);
+      // nothing of this block may still be in flight when it exits: no copy, and no arrival of a product's completion
+      for (int i = max(0, issued - Sm::NS); i < issued; i++) {
+        mbar_wait(&misc->full[i % Sm::NS], (i / Sm::NS) & 1, abortp, status, false);
+        mbar_wait(&misc->empty[i % Sm::NS], (i / Sm::NS) & 1, abortp, status);
+      }
     }
   } else if (warp == CXW_MMA) {
-    // The whole warp walks the schedule (waits and descriptor arithmetic stay warp-uniform); an elected lane issues.
-    constexpr uint32_t ID_S = idesc_bf16(128, 128, 0, 0);
-    const uint32_t ID_O = idesc_bf16(128, a.dv, 0, 1);
-    const uint32_t sQ = smem_u32(sm + Sm::Q), sR = smem_u32(sm + Sm::RING);
+    // The whole warp walks the schedule (waits and descriptor arithmetic stay warp-uniform); an elected lane issues.  (One warp for
+    // both warpgroups: with one each, whose short products then alternate on the tensor pipe, 677 us became 714 and 228 us 290.)
+    const uint32_t ID_S = idesc_bf16(128, KT, 0, 0), ID_O = idesc_bf16(128, a.dv, 0, 1);
+    const uint32_t sR = smem_u32(sm + Sm::RING);
     const int ksteps = a.d / 16;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abortp, status)) != 0; };
-    auto issue_s = [&](int i) {                        // S of item i
-      const int w = i & 1, t = both ? i >> 1 : i, slot = 2 * t % Sm::NS;
-      if (!wait(&misc->full[slot], (2 * t / Sm::NS) & 1)) return false;
+    const Desc q0 = smem_desc(smem_u32(sm + Sm::Q), 16, 1024, SWZ_128B), k0 = smem_desc(sR, 16, 1024, SWZ_128B), v0 = smem_desc(sR, Sm::PANEL, 1024, SWZ_128B);
+    const bool leader = elect_one();
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, abortp, status); };
+    int kslot = 0, kphase = 0, vslot = 1, vphase = 0;      // where the next K and V tiles are
+    auto issue_s = [&](int w) {                        // S of the next item, which is warpgroup w's
+      if (!wait(&misc->full[kslot], kphase)) return false;
       tcgen05_fence_after();
-      const uint64_t dQ = smem_desc(sQ + (both ? w : 0) * Sm::SLOT, 16, 1024, SWZ_128B), dK = smem_desc(sR + slot * Sm::SLOT, 16, 1024, SWZ_128B);
-      if (elect_one()) {
-        for (int k = 0; k < ksteps; k++) {
-          const uint32_t off = (k >> 2) * TILE_BYTES + (k & 3) * 32;
-          mma_bf16(tmem + CX_S + w * 128, desc_advance(dQ, off), desc_advance(dK, off), ID_S, k > 0);
-        }
-        if (!both || w) mma_commit(&misc->empty[slot]);
+      if (leader) {
+        Desc q = q0, k = k0;
+        q.lo += (both ? w : 0) * (Sm::QT / 16);
+        k.lo += kslot * (Sm::SLOT / 16);
+        issue_rows<D / 16, TILE_BYTES, Sm::PANEL>(tmem + w * Sm::GROUP + Sm::S, q, k, ID_S, ksteps);
+        if (!both || w) mma_commit(&misc->empty[kslot]);
         mma_commit(&misc->s_full[w]);
       }
       __syncwarp();
+      if (!both || w) {
+        kslot += 2;
+        if (kslot >= Sm::NS) { kslot -= Sm::NS; kphase ^= 1; }
+      }
       return true;
     };
     bool ok = nt > 0 && wait(&misc->q_ready, 0);
-    if (ok) {
+    if (ok) ok = issue_s(0) && (items < 2 || issue_s(1));
+    auto item = [&](int i, int w) {
+      // S of the item after the next, as soon as the scores that lie there have been read
+      if (!Sm::OVER && i + 2 < items && (!wait(&misc->s_free[w], (i >> 1) & 1) || !issue_s(w))) return false;
+      if (!wait(&misc->full[vslot], vphase) || !wait(&misc->p_ready[w], (i >> 1) & 1)) return false;
       tcgen05_fence_after();
-      ok = issue_s(0) && (items < 2 || issue_s(1));
-    }
-    for (int i = 0; i < items && ok; i++) {
-      const int w = i & 1, t = both ? i >> 1 : i, slot = (2 * t + 1) % Sm::NS;
-      ok = wait(&misc->full[slot], ((2 * t + 1) / Sm::NS) & 1) && wait(&misc->p_ready[w], (i >> 1) & 1);
-      if (!ok) break;
-      tcgen05_fence_after();
-      // V: panels of 64 columns (leading offset = their distance), 16 keys per step = 16 rows of 128 bytes
-      const uint64_t dV = smem_desc(sR + slot * Sm::SLOT, TILE_BYTES, 1024, SWZ_128B);
-      if (elect_one()) {
-#pragma unroll
-        for (int k = 0; k < 8; k++)
-          mma_bf16_ta(tmem + CX_O + w * 128, tmem + CX_S + w * 128 + 8 * k, desc_advance(dV, k * 2048), ID_O, i > 1 || k > 0);
-        if (!both || w) mma_commit(&misc->empty[slot]);
-        if (i + 2 >= items) mma_commit(&misc->o_full[w]);
+      if (leader) {
+        // V: panels of 64 columns (leading offset = their distance), 16 keys per step = 16 rows of 128 bytes
+        Desc v = v0;
+        v.lo += vslot * (Sm::SLOT / 16);
+        issue_cols<KT / 16>(tmem + w * Sm::GROUP + Sm::O, tmem + w * Sm::GROUP + Sm::P, v, ID_O, i > 1);
+        if (!both || w) mma_commit(&misc->empty[vslot]);
+        mma_commit(&misc->o_full[w]);
       }
       __syncwarp();
-      if (i + 2 < items) ok = issue_s(i + 2);
-    }
+      if (!both || w) {
+        vslot += 2;
+        if (vslot >= Sm::NS) { vslot -= Sm::NS; vphase ^= 1; }
+      }
+      return !Sm::OVER || i + 2 >= items || issue_s(w);
+    };
+    for (int i = 0; i < items && ok; i += 2) ok = item(i, 0) && (i + 1 >= items || item(i + 1, 1));
   } else if (warp < CX_WARPS) {
-    regs_acquire<REGS_EPILOGUE>();
+    regs_acquire<CX_REGS_ROWS>();
     const int w = warp >> 2, row = (warp & 3) * 32 + lane;
     {
       // the block's rows of Q into shared memory, rows and columns that there are none of as zeros
@@ -151,12 +172,12 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         const int rr = i / CH, ch = i % CH, r = r0 + rr;
         uint4 x = make_uint4(0, 0, 0, 0);
         if (r < R && ch * 8 < a.d) x = *reinterpret_cast<const uint4*>(Q + (int64_t)(hk * a.g + r / a.Lq) * a.aq.sh + (int64_t)(r % a.Lq) * a.aq.sl + ch * 8);
-        *reinterpret_cast<uint4*>(sm + Sm::Q + (rr >> 7) * Sm::SLOT + (ch >> 3) * TILE_BYTES + sw128_offset(rr & 127, (ch & 7) * 8)) = x;
+        *reinterpret_cast<uint4*>(sm + Sm::Q + (rr >> 7) * Sm::QT + (ch >> 3) * TILE_BYTES + sw128_offset(rr & 127, (ch & 7) * 8)) = x;
       }
       fence_proxy_async_smem();
       mbar_arrive_warp(&misc->q_ready, lane);
     }
-    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), tS = lanes + CX_S + w * 128, tO = lanes + CX_O + w * 128;
+    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), tS = lanes + w * Sm::GROUP + Sm::S, tP = lanes + w * Sm::GROUP + Sm::P, tO = lanes + w * Sm::GROUP + Sm::O;
     const int first = r0 + (both ? w * TILE : 0), r = first + row;      // this thread's row
     const bool idle = first + (warp & 3) * 32 >= R;                     // no row of this warp exists
     const int mine = both ? nt : (nt + 1 - w) / 2;                      // its tiles
@@ -165,21 +186,21 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     uint32_t l[2] = {0u, 0u};
     bool ok = true;
     for (int i = 0; i < mine; i++) {
-      const int t = both ? i : 2 * i + w, j0 = (t0 + t) * TILE;
-      uint32_t seen[4];
-      const bool some = a.key_mask != nullptr || j0 + TILE > n;         // some key of the tile may be hidden
+      const int t = both ? i : 2 * i + w, j0 = (t0 + t) * KT;
+      uint32_t seen[KT / 32];
+      const bool some = a.key_mask != nullptr || j0 + KT > n;           // some key of the tile may be hidden
       if (some) {
 #pragma unroll
-        for (int q = 0; q < 4; q++) seen[q] = __ballot_sync(0xffffffffu, cross_seen(a, b, j0 + q * 32 + lane, n));
+        for (int q = 0; q < KT / 32; q++) seen[q] = __ballot_sync(0xffffffffu, cross_seen(a, b, j0 + q * 32 + lane, n));
         if (!both || w == 0) {
           // what a hidden key's V holds may be anything: zeros in its place, thread = key (one warpgroup does it for both: the
           // other's product is issued behind its own)
           const int slot = (2 * t + 1) % Sm::NS;
           ok = __all_sync(0xffffffffu, mbar_wait(&misc->full[slot], ((2 * t + 1) / Sm::NS) & 1, abortp, status, false));
-          if (ok && !(seen[warp & 3] >> lane & 1u))
+          if (ok && row < KT && !(seen[(warp & 3) % (KT / 32)] >> lane & 1u))
             for (int p = 0; p < vp; p++)
               for (int k = 0; k < 8; k++)
-                *reinterpret_cast<uint4*>(sm + Sm::RING + slot * Sm::SLOT + p * TILE_BYTES + row * 128 + k * 16) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4*>(sm + Sm::RING + slot * Sm::SLOT + p * Sm::PANEL + row * 128 + k * 16) = make_uint4(0, 0, 0, 0);
           fence_proxy_async_smem();
         }
       }
@@ -187,32 +208,42 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       if (!ok) break;
       tcgen05_fence_after();
       if (!idle) {
-        uint32_t s[128];
+        uint32_t s[KT];
 #pragma unroll
-        for (int q = 0; q < 8; q++) tmem_ld16(tS + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(s + 16 * q));
+        for (int q = 0; q < KT; q += 16) tmem_ld16(tS + q, *reinterpret_cast<uint32_t(*)[16]>(s + q));
         tmem_wait_ld();
+        if (!Sm::OVER) {
+          tcgen05_fence_before();
+          mbar_arrive_warp(&misc->s_free[w], lane);
+        }
         if (some) {
 #pragma unroll
-          for (int q = 0; q < 128; q++) s[q] = (seen[q >> 5] >> (q & 31)) & 1u ? s[q] : 0xff800000u;
+          for (int q = 0; q < KT; q++) s[q] = (seen[q >> 5] >> (q & 31)) & 1u ? s[q] : 0xff800000u;
         }
         float top = __uint_as_float(s[0]);
         {
           float t1 = __uint_as_float(s[1]), t2 = __uint_as_float(s[2]), t3 = __uint_as_float(s[3]);
 #pragma unroll
-          for (int q = 4; q < 124; q += 8) {
+          for (int q = 4; q < KT - 4; q += 8) {
             top = max3n(top, __uint_as_float(s[q]), __uint_as_float(s[q + 1]));
             t1 = max3n(t1, __uint_as_float(s[q + 2]), __uint_as_float(s[q + 3]));
             t2 = max3n(t2, __uint_as_float(s[q + 4]), __uint_as_float(s[q + 5]));
             t3 = max3n(t3, __uint_as_float(s[q + 6]), __uint_as_float(s[q + 7]));
           }
-          top = max3n(top, __uint_as_float(s[124]), __uint_as_float(s[125]));
-          t1 = max3n(t1, __uint_as_float(s[126]), __uint_as_float(s[127]));
+          top = max3n(top, __uint_as_float(s[KT - 4]), __uint_as_float(s[KT - 3]));
+          t1 = max3n(t1, __uint_as_float(s[KT - 2]), __uint_as_float(s[KT - 1]));
           top = max3n(max3n(top, t1, t2), t3, t3);
         }
         top *= c;
         // (an infinite score makes the row NaN as its definition does: the cubic below would drop inf - inf)
         if (top == INFINITY) top = __uint_as_float(0x7fc00000u);
         const bool grown = !(top <= m + CX_SLACK) && top != -INFINITY;
+        // the product that reads P and adds to O is done (OVER: S came behind it)
+        if (!Sm::OVER && i > 0) {
+          ok = __all_sync(0xffffffffu, mbar_wait(&misc->o_full[w], (i - 1) & 1, abortp, status, false));
+          if (!ok) break;
+          tcgen05_fence_after();
+        }
         if (__any_sync(0xffffffffu, grown)) {
           const float f = grown ? ex2(m - top) : 1.f;
           if (grown) m = top;
@@ -231,12 +262,12 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         }
         const float base = m == -INFINITY ? 0.f : -m;
 #pragma unroll
-        for (int q = 0; q < 128; q += 32) {
+        for (int q = 0; q < KT; q += 32) {
           uint32_t o[16];
 #pragma unroll
           for (int k = 0; k < 32; k += 2) {
             fma2(s[q + k], s[q + k + 1], c, base);
-            if ((k & 7) < 4) {
+            if ((k & 15) < 16 - 2 * CX_CUBIC) {
               s[q + k] = __float_as_uint(ex2(__uint_as_float(s[q + k])));
               s[q + k + 1] = __float_as_uint(ex2(__uint_as_float(s[q + k + 1])));
             } else {
@@ -245,16 +276,21 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             add2(l[0], l[1], __uint_as_float(s[q + k]), __uint_as_float(s[q + k + 1]));
             o[k / 2] = pack_bf16(__uint_as_float(s[q + k]), __uint_as_float(s[q + k + 1]));
           }
-          tmem_st16(tS + q / 2, o);
+          tmem_st16(tP + q / 2, o);
         }
         tmem_wait_st();
+      } else {
+        if (!Sm::OVER) mbar_arrive_warp(&misc->s_free[w], lane);
+        // (in step with the warps that have rows: an arrival below belongs to this tile's product)
+        ok = Sm::OVER || i == 0 || __all_sync(0xffffffffu, mbar_wait(&misc->o_full[w], (i - 1) & 1, abortp, status, false));
+        if (!ok) break;
       }
       tcgen05_fence_before();
       mbar_arrive_warp(&misc->p_ready[w], lane);
     }
     // all products are done before anything of the ring is written below
-    if (ok && mine > 0) ok = mbar_wait(&misc->o_full[w], 0, abortp, status, false);
-    if (ok && !both && (nt + w) / 2 > 0) ok = mbar_wait(&misc->o_full[w ^ 1], 0, abortp, status, false);
+    if (ok && mine > 0) ok = mbar_wait(&misc->o_full[w], (mine - 1) & 1, abortp, status, false);
+    if (!both) named_bar_sync(3, 256);                  // (the other warpgroup's, too)
     ok = __all_sync(0xffffffffu, ok);
     tcgen05_fence_after();
     float sum = m == -INFINITY ? 0.f : __uint_as_float(l[0]) + __uint_as_float(l[1]);      // (2^-125 per hidden key from the cubic)
@@ -359,18 +395,19 @@ int fs_tc_cross_map(CUtensorMap* map, const void* base, TensorAddr t, int B, int
   return tchost::make_map_rows(map, base, t, B, H, L, inner, rows);
 }
 
-// Pieces that bring the blocks up to one per SM, each with two tiles at least.
+// Pieces that bring the blocks up to what is resident at once, each with 256 keys at least.
 int fs_tc_cross_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm) {
-  const int64_t R = (int64_t)dm->H / dm->Hk * dm->Lq, blocks = (int64_t)dm->B * dm->Hk * ((R + 255) / 256), tiles = ((int64_t)dm->Lk + TILE - 1) / TILE;
+  const int64_t R = (int64_t)dm->H / dm->Hk * dm->Lq, blocks = (int64_t)dm->B * dm->Hk * ((R + 255) / 256), some = ((int64_t)dm->Lk + 255) / 256;
   int64_t p = ctx->sm_count / blocks;
-  if (p > tiles / 2) p = tiles / 2;
+  if (p > some) p = some;
   if (p > 64) p = 64;
   return p < 1 ? 1 : (int)p;
 }
 
 int fs_tc_cross(fsharp_ctx* ctx, const CrossArgs& a, void* Y, TensorAddr ay, float* lse, CrossPart part) {
   CUtensorMap tmK, tmV;
-  FS_TRY(fs_tc_cross_map(&tmK, a.K, a.ak, a.B, a.Hk, a.Lk, a.d, TILE));
-  FS_TRY(fs_tc_cross_map(&tmV, a.V, a.av, a.B, a.Hk, a.Lk, a.dv, TILE));
+  const int rows = a.d > 64 || a.dv > 64 ? CxSm<128>::KT : CxSm<64>::KT;
+  FS_TRY(fs_tc_cross_map(&tmK, a.K, a.ak, a.B, a.Hk, a.Lk, a.d, rows));
+  FS_TRY(fs_tc_cross_map(&tmV, a.V, a.av, a.B, a.Hk, a.Lk, a.dv, rows));
   return a.d > 64 || a.dv > 64 ? launch<128>(ctx, tmK, tmV, a, Y, ay, lse, part) : launch<64>(ctx, tmK, tmV, a, Y, ay, lse, part);
 }

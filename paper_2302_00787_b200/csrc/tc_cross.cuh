@@ -33,4 +33,26 @@ __device__ __forceinline__ void addmul2(uint32_t& a, uint32_t& b, float n, float
       : "f"(n), "f"(o), "r"(p), "r"(q));
 }
 
+// The products' issue.  One elected lane issues; what it takes to say a product (two descriptors, two addresses) has to be a
+// constant away from a value that the warp holds, or the issue of a tile's few short products takes longer than the products:
+// the loop below is unrolled, with the steps that d has not (d < D) left out by a warp-uniform branch.
+struct Desc {
+  uint32_t lo, hi;
+  __device__ __forceinline__ Desc(uint64_t d) : lo((uint32_t)d), hi((uint32_t)(d >> 32)) {}
+};
+// D [128 x N] = A [128 x 16 steps] B [N x 16 steps]^T, both K-major in panels of 64 columns of A_PANEL and B_PANEL bytes
+template <int STEPS, uint32_t A_PANEL, uint32_t B_PANEL>
+__device__ __forceinline__ void issue_rows(uint32_t d_tmem, Desc a, Desc b, uint32_t idesc, int steps) {
+#pragma unroll
+  for (int k = 0; k < STEPS; k++)
+    if (k < steps)
+      tc::mma_bf16_lh(d_tmem, a.lo + ((k >> 2) * A_PANEL + (k & 3) * 32) / 16, a.hi, b.lo + ((k >> 2) * B_PANEL + (k & 3) * 32) / 16, b.hi, idesc, k > 0);
+}
+// D [128 x N] (+)= A [128 x 16 STEPS] in tensor memory times B, whose 16 STEPS rows (of 128 bytes per panel) are the contraction
+template <int STEPS>
+__device__ __forceinline__ void issue_cols(uint32_t d_tmem, uint32_t a_tmem, Desc b, uint32_t idesc, uint32_t accumulate) {
+#pragma unroll
+  for (int k = 0; k < STEPS; k++) tc::mma_bf16_ta_lh(d_tmem, a_tmem + 8 * k, b.lo + k * (2048 / 16), b.hi, idesc, k > 0 ? 1u : accumulate);
+}
+
 }  // namespace tcx

@@ -102,50 +102,57 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           tma_load_4d(base + Sm::SLOT + p * HALF_BYTES, &tmG, &misc->full[s], p * 64, t * HALF, gr.ady.sh ? h : 0, gr.ady.sb ? b : 0);
         bulk_load(sm + Sm::STAT + s * 512, gr.stat + ((int64_t)b * a.H + h) * cross_stat_floats(a.Lq) + (int64_t)t * 128, 512, &misc->full[s]);
       }
-      // no copy of this block may still be in flight when it exits
+      // nothing of this block may still be in flight when it exits: no copy, and no arrival of a product's completion
       mbar_wait(&misc->kv_full, 0, abortp, status, false);
-      for (int k = max(0, i - Sm::NS); k < i; k++) mbar_wait(&misc->full[k % Sm::NS], (k / Sm::NS) & 1, abortp, status, false);
+      for (int k = max(0, i - Sm::NS); k < i; k++) {
+        mbar_wait(&misc->full[k % Sm::NS], (k / Sm::NS) & 1, abortp, status, false);
+        mbar_wait(&misc->empty[k % Sm::NS], (k / Sm::NS) & 1, abortp, status);
+      }
     }
   } else if (warp == CGW_MMA) {
     constexpr uint32_t ID_S = idesc_bf16(128, HALF, 0, 0);
     const uint32_t ID_V = idesc_bf16(128, a.dv, 0, 1), ID_K = idesc_bf16(128, a.d, 0, 1);
     const uint32_t sR = smem_u32(sm + Sm::RING);
-    const uint64_t dK = smem_desc(smem_u32(sm + Sm::K), 16, 1024, SWZ_128B), dV = smem_desc(smem_u32(sm + Sm::V), 16, 1024, SWZ_128B);
+    const Desc k0 = smem_desc(smem_u32(sm + Sm::K), 16, 1024, SWZ_128B), v0 = smem_desc(smem_u32(sm + Sm::V), 16, 1024, SWZ_128B);
+    const Desc q0 = smem_desc(sR, 16, 1024, SWZ_128B), qt = smem_desc(sR, HALF_BYTES, 1024, SWZ_128B);      // dY: a slot behind Q
     const int ks = a.d / 16, vs = a.dv / 16;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abortp, status)) != 0; };
-    auto issue_sp = [&](int i) {                       // S^T and dP^T of tile i
-      const int s = i % Sm::NS, w = i & 1;
-      if (!wait(&misc->full[s], (i / Sm::NS) & 1)) return false;
+    const bool leader = elect_one();
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, abortp, status); };
+    int slot = 0, phase = 0, done = 0;                 // the next tile's stage; the stage of the tile whose sums come next
+    auto issue_sp = [&](int w) {                       // S^T and dP^T of the next tile, which is warpgroup w's
+      if (!wait(&misc->full[slot], phase)) return false;
       tcgen05_fence_after();
-      const uint64_t dQ = smem_desc(sR + s * Sm::STAGE, 16, 1024, SWZ_128B), dG = smem_desc(sR + s * Sm::STAGE + Sm::SLOT, 16, 1024, SWZ_128B);
-      if (elect_one()) {
-        for (int k = 0; k < ks; k++)
-          mma_bf16(tmem + w * 128, desc_advance(dK, (k >> 2) * TILE_BYTES + (k & 3) * 32), desc_advance(dQ, (k >> 2) * HALF_BYTES + (k & 3) * 32), ID_S, k > 0);
-        for (int k = 0; k < vs; k++)
-          mma_bf16(tmem + w * 128 + 64, desc_advance(dV, (k >> 2) * TILE_BYTES + (k & 3) * 32), desc_advance(dG, (k >> 2) * HALF_BYTES + (k & 3) * 32), ID_S, k > 0);
+      if (leader) {
+        Desc q = q0;
+        q.lo += slot * (Sm::STAGE / 16);
+        issue_rows<D / 16, TILE_BYTES, HALF_BYTES>(tmem + w * 128, k0, q, ID_S, ks);
+        q.lo += Sm::SLOT / 16;
+        issue_rows<D / 16, TILE_BYTES, HALF_BYTES>(tmem + w * 128 + 64, v0, q, ID_S, vs);
         mma_commit(&misc->sp_full[w]);
       }
       __syncwarp();
+      if (++slot == Sm::NS) { slot = 0; phase ^= 1; }
       return true;
     };
     bool ok = items > 0 && wait(&misc->kv_full, 0) && issue_sp(0) && (items < 2 || issue_sp(1));
-    for (int i = 0; i < items && ok; i++) {
-      const int s = i % Sm::NS, w = i & 1;
-      if (!(ok = wait(&misc->ready[w], (i >> 1) & 1))) break;
+    auto item = [&](int i, int w) {
+      if (!wait(&misc->ready[w], (i >> 1) & 1)) return false;
       tcgen05_fence_after();
-      // Q and dY again, now with their rows as the contraction: panels of 64 columns, 16 rows of 128 bytes per step
-      const uint64_t dQ = smem_desc(sR + s * Sm::STAGE, HALF_BYTES, 1024, SWZ_128B), dG = smem_desc(sR + s * Sm::STAGE + Sm::SLOT, HALF_BYTES, 1024, SWZ_128B);
-      if (elect_one()) {
-#pragma unroll
-        for (int k = 0; k < 4; k++) mma_bf16_ta(tmem + CG_SUM, tmem + w * 128 + 8 * k, desc_advance(dG, k * 2048), ID_V, i > 0 || k > 0);
-#pragma unroll
-        for (int k = 0; k < 4; k++) mma_bf16_ta(tmem + CG_SUM + D, tmem + w * 128 + 64 + 8 * k, desc_advance(dQ, k * 2048), ID_K, i > 0 || k > 0);
-        mma_commit(&misc->empty[s]);
+      if (leader) {
+        // Q and dY again, now with their rows as the contraction: panels of 64 columns, 16 rows of 128 bytes per step
+        Desc q = qt;
+        q.lo += done * (Sm::STAGE / 16);
+        issue_cols<4>(tmem + CG_SUM + D, tmem + w * 128 + 64, q, ID_K, i > 0);
+        q.lo += Sm::SLOT / 16;
+        issue_cols<4>(tmem + CG_SUM, tmem + w * 128, q, ID_V, i > 0);
+        mma_commit(&misc->empty[done]);
         if (i == items - 1) mma_commit(&misc->done);
       }
       __syncwarp();
-      if (i + 2 < items) ok = issue_sp(i + 2);
-    }
+      if (++done == Sm::NS) done = 0;
+      return i + 2 >= items || issue_sp(w);
+    };
+    for (int i = 0; i < items && ok; i += 2) ok = item(i, 0) && (i + 1 >= items || item(i + 1, 1));
   } else if (warp < CG_WARPS) {
     regs_acquire<REGS_EPILOGUE>();
     const int w = warp >> 2, row = (warp & 3) * 32 + lane;
@@ -293,29 +300,37 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         for (int p = 0; p < kp; p++) tma_load_4d(base + p * HALF_BYTES, &tmK, &misc->full[s], p * 64, tok, a.ak.sh ? hk : 0, a.ak.sb ? b : 0);
         for (int p = 0; p < vp; p++) tma_load_4d(base + Sm::SLOT + p * HALF_BYTES, &tmV, &misc->full[s], p * 64, tok, a.av.sh ? hk : 0, a.av.sb ? b : 0);
       }
-      // no copy of this block may still be in flight when it exits
-      for (int k = max(0, i - Sm::NS); k < i; k++) mbar_wait(&misc->full[k % Sm::NS], (k / Sm::NS) & 1, abortp, status, false);
+      // nothing of this block may still be in flight when it exits: no copy, and no arrival of a product's completion
+      for (int k = max(0, i - Sm::NS); k < i; k++) {
+        mbar_wait(&misc->full[k % Sm::NS], (k / Sm::NS) & 1, abortp, status, false);
+        mbar_wait(&misc->empty[k % Sm::NS], (k / Sm::NS) & 1, abortp, status);
+      }
     }
   } else if (warp == CGW_MMA) {
     constexpr uint32_t ID_S = idesc_bf16(128, HALF, 0, 0);
     const uint32_t ID_Q = idesc_bf16(128, a.d, 0, 1);
     const uint32_t sR = smem_u32(sm + Sm::RING), sQ = smem_u32(sm + Sm::Q), sG = smem_u32(sm + Sm::G);
     const int ks = a.d / 16, vs = a.dv / 16;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abortp, status)) != 0; };
-    auto issue_sp = [&](int i) {                       // S and dP of item i
-      const int w = i & 1, t = both ? i >> 1 : i, s = t % Sm::NS;
-      if (!wait(&misc->full[s], (t / Sm::NS) & 1)) return false;
+    const Desc q0 = smem_desc(sQ, 16, 1024, SWZ_128B), g0 = smem_desc(sG, 16, 1024, SWZ_128B);
+    const Desc k0 = smem_desc(sR, 16, 1024, SWZ_128B), kt = smem_desc(sR, HALF_BYTES, 1024, SWZ_128B);      // V: a slot behind K
+    const bool leader = elect_one();
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, abortp, status); };
+    int slot = 0, phase = 0, done = 0;                 // the next tile's stage; the stage of the tile whose sums come next
+    auto issue_sp = [&](int w) {                       // S and dP of the next item, which is warpgroup w's
+      if (!wait(&misc->full[slot], phase)) return false;
       tcgen05_fence_after();
-      const uint64_t dK = smem_desc(sR + s * Sm::STAGE, 16, 1024, SWZ_128B), dV = smem_desc(sR + s * Sm::STAGE + Sm::SLOT, 16, 1024, SWZ_128B);
-      const uint64_t dQ = smem_desc(sQ + (both ? w : 0) * Sm::BIG, 16, 1024, SWZ_128B), dG = smem_desc(sG + (both ? w : 0) * Sm::BIG, 16, 1024, SWZ_128B);
-      if (elect_one()) {
-        for (int k = 0; k < ks; k++)
-          mma_bf16(tmem + w * 128, desc_advance(dQ, (k >> 2) * TILE_BYTES + (k & 3) * 32), desc_advance(dK, (k >> 2) * HALF_BYTES + (k & 3) * 32), ID_S, k > 0);
-        for (int k = 0; k < vs; k++)
-          mma_bf16(tmem + w * 128 + 64, desc_advance(dG, (k >> 2) * TILE_BYTES + (k & 3) * 32), desc_advance(dV, (k >> 2) * HALF_BYTES + (k & 3) * 32), ID_S, k > 0);
+      if (leader) {
+        Desc q = q0, g = g0, k = k0;
+        q.lo += (both ? w : 0) * (Sm::BIG / 16);
+        g.lo += (both ? w : 0) * (Sm::BIG / 16);
+        k.lo += slot * (Sm::STAGE / 16);
+        issue_rows<D / 16, TILE_BYTES, HALF_BYTES>(tmem + w * 128, q, k, ID_S, ks);
+        k.lo += Sm::SLOT / 16;
+        issue_rows<D / 16, TILE_BYTES, HALF_BYTES>(tmem + w * 128 + 64, g, k, ID_S, vs);
         mma_commit(&misc->sp_full[w]);
       }
       __syncwarp();
+      if ((!both || w) && ++slot == Sm::NS) { slot = 0; phase ^= 1; }
       return true;
     };
     bool ok = nt > 0 && wait(&misc->q_ready, 0);
@@ -323,20 +338,21 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       tcgen05_fence_after();
       ok = issue_sp(0) && (items < 2 || issue_sp(1));
     }
-    for (int i = 0; i < items && ok; i++) {
-      const int w = i & 1, t = both ? i >> 1 : i, s = t % Sm::NS;
-      if (!(ok = wait(&misc->ready[w], (i >> 1) & 1))) break;
+    auto item = [&](int i, int w) {
+      if (!wait(&misc->ready[w], (i >> 1) & 1)) return false;
       tcgen05_fence_after();
-      const uint64_t dK = smem_desc(sR + s * Sm::STAGE, HALF_BYTES, 1024, SWZ_128B);      // its keys as the contraction
-      if (elect_one()) {
-#pragma unroll
-        for (int k = 0; k < 4; k++) mma_bf16_ta(tmem + CG_SUM + w * 128, tmem + w * 128 + 8 * k, desc_advance(dK, k * 2048), ID_Q, i > 1 || k > 0);
-        if (!both || w) mma_commit(&misc->empty[s]);
+      if (leader) {
+        Desc k = kt;                                   // its keys as the contraction
+        k.lo += done * (Sm::STAGE / 16);
+        issue_cols<4>(tmem + CG_SUM + w * 128, tmem + w * 128, k, ID_Q, i > 1);
+        if (!both || w) mma_commit(&misc->empty[done]);
         if (i + 2 >= items) mma_commit(&misc->done[w]);
       }
       __syncwarp();
-      if (i + 2 < items) ok = issue_sp(i + 2);
-    }
+      if ((!both || w) && ++done == Sm::NS) done = 0;
+      return i + 2 >= items || issue_sp(w);
+    };
+    for (int i = 0; i < items && ok; i += 2) ok = item(i, 0) && (i + 1 >= items || item(i + 1, 1));
   } else if (warp < CG_WARPS) {
     regs_acquire<REGS_EPILOGUE>();
     const int w = warp >> 2, row = (warp & 3) * 32 + lane;

@@ -115,7 +115,7 @@ def test_binding_refuses_what_the_kernels_would_overrun(lib, blank):
         ctx.fsharp_rotate(x, x, fb.make_rope(32))
     with pytest.raises(ValueError):
         ctx.fsharp_cross_attend(x, x, x)
-    ctx._mine = lambda *named: None                                   # (what stands behind the check of the device)
+    ctx._mine = lambda **named: None                                  # (what stands behind the check of the device)
     with pytest.raises(ValueError):
         ctx.fsharp_rotate(x, x[:, :, :4], fb.make_rope(32))
     with pytest.raises(ValueError):
