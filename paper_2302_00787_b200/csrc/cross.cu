@@ -6,14 +6,14 @@
 
 namespace {
 
-// -lse log2(e) and -D, D = dY . Y, of every row and of the places up to a multiple of 64 (cross.cuh).  dv / VE lanes share a
+// -lse log2(e) and -D, D = dY . Y, of every row and of the places up to a multiple of 128 (cross.cuh).  dv / VE lanes share a
 // row's dv values, 16 bytes each.
 template <typename T>
 __global__ void __launch_bounds__(256)
 cross_delta_kernel(const T* __restrict__ Y, TensorAddr ay, const T* __restrict__ dY, TensorAddr ady, const float* __restrict__ lse,
                    int64_t places, int H, int Lq, int dv, float* __restrict__ stat) {
   constexpr int VE = 16 / (int)sizeof(T);
-  const int lpr = dv / VE, Lp = (Lq + 63) / 64 * 64;  // lpr: 2 .. 32, a power of two
+  const int lpr = dv / VE, Lp = (Lq + 127) / 128 * 128;  // lpr: 2 .. 32, a power of two
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, place = i / lpr, bh = place / Lp;
   const int e = (int)(i % lpr) * VE, tok = (int)(place % Lp);
   const bool row = place < places && tok < Lq;
@@ -29,9 +29,9 @@ cross_delta_kernel(const T* __restrict__ Y, TensorAddr ay, const T* __restrict__
   for (int w = 1; w < lpr; w <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
   if (place < places && e == 0) {
     const float x = row ? lse[bh * Lq + tok] : -INFINITY;
-    float* to = stat + bh * cross_stat_floats(Lq) + (int64_t)(tok >> 6) * 128 + (tok & 63);
+    float* to = stat + bh * cross_stat_floats(Lq) + (int64_t)(tok >> 7) * 256 + (tok & 127);
     to[0] = x == -INFINITY ? -INFINITY : -x * FS_LOG2E;
-    to[64] = row ? -sum : 0.f;
+    to[128] = row ? -sum : 0.f;
   }
 }
 
@@ -57,7 +57,7 @@ cross_sum_kernel(const float* __restrict__ part, int pieces, int64_t rows, int l
 
 template <typename T>
 int run_delta(fsharp_ctx* ctx, const CrossArgs& a, const void* Y, TensorAddr ay, const void* dY, TensorAddr ady, const float* lse, float* stat) {
-  const int64_t places = (int64_t)a.B * a.H * (((int64_t)a.Lq + 63) / 64 * 64), blocks = (places * (a.dv * (int64_t)sizeof(T) / 16) + 255) / 256;
+  const int64_t places = (int64_t)a.B * a.H * (((int64_t)a.Lq + 127) / 128 * 128), blocks = (places * (a.dv * (int64_t)sizeof(T) / 16) + 255) / 256;
   if (blocks > 0x7fffffff) return FSHARP_E_SHAPE;
   FS_TIME_BEGIN(ctx, FS_K_CROSS_DELTA);
   cross_delta_kernel<T><<<(unsigned)blocks, 256, 0, ctx->stream>>>(static_cast<const T*>(Y), ay, static_cast<const T*>(dY), ady, lse, places,

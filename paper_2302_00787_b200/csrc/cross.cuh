@@ -46,7 +46,7 @@ int fs_cross_join(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, Tenso
 int fs_cross_fma_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm);
 int fs_cross_fma(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, TensorAddr ay, float* lse, CrossPart part);
 
-// Backward.  stat [B][H][ceil(Lq / 64)][2][64]: 64 rows' -lse log2(e), then their -D; rows that see nothing and places behind the last
+// Backward.  stat [B][H][ceil(Lq / 128)][2][128]: 128 rows' -lse log2(e), then their -D; rows that see nothing and places behind the last
 // row have -inf and 0, which makes every 2^(x - lse) of theirs zero.  Partial sums of a piece: dK | dV [piece][unit][Lk][d + dv], dQ [piece][unit][R][d].
 struct CrossGrad {
   const void* dY;
@@ -57,11 +57,11 @@ struct CrossGrad {
   float *pkv, *pq;             // null where the one piece writes the gradients themselves
   int kv_pieces, q_pieces;
 };
-__host__ __device__ __forceinline__ int64_t cross_stat_floats(int Lq) { return ((int64_t)Lq + 63) / 64 * 128; }
+__host__ __device__ __forceinline__ int64_t cross_stat_floats(int Lq) { return ((int64_t)Lq + 127) / 128 * 256; }
 // (-lse log2(e), -D) of token i of (batch, head) bh
 __device__ __forceinline__ float2 cross_stat(const float* stat, int64_t bh, int Lq, int i) {
-  const float* p = stat + bh * cross_stat_floats(Lq) + (int64_t)(i >> 6) * 128 + (i & 63);
-  return make_float2(p[0], p[64]);
+  const float* p = stat + bh * cross_stat_floats(Lq) + (int64_t)(i >> 7) * 256 + (i & 127);
+  return make_float2(p[0], p[128]);
 }
 // tensor cores (tc_cross_bwd.cu): bf16
 void fs_tc_cross_grad_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int* kv_pieces, int* q_pieces);

@@ -13,10 +13,6 @@ constexpr int RW_T = 128, RW_WARPS = RW_T / 32, RW_U = 4, RW_STAGES = 3;
 constexpr size_t RW_RING = (size_t)RW_STAGES * 2 * RW_U * RW_T * 16;      // 48 KB: four blocks on an SM
 constexpr int RW_CLUSTER = 8;      // most pieces that meet in a cluster
 
-// 16 bytes into shared memory behind the registers' back, zeros where there is nothing to read
-__device__ __forceinline__ void copy16(uint4* to, const void* from, bool some) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(to)), "l"(from), "r"(some ? 16 : 0) : "memory");
-}
 template <typename T> __device__ __forceinline__ void widen(const uint4& x, float* v);
 template <> __device__ __forceinline__ void widen<float>(const uint4& x, float* v) {
   v[0] = __uint_as_float(x.x); v[1] = __uint_as_float(x.y); v[2] = __uint_as_float(x.z); v[3] = __uint_as_float(x.w);
@@ -72,8 +68,8 @@ cross_rows_kernel(const __grid_constant__ CrossArgs a, T* __restrict__ Y, Tensor
 #pragma unroll
       for (int u = 0; u < RW_U; u++) {
         const int64_t j = t * STEP + (u * RW_WARPS + warp) * KPW + grp;
-        copy16(to + 2 * u * RW_T, Kb + (j < n ? j * a.ak.sl : 0), j < n && inq);
-        copy16(to + (2 * u + 1) * RW_T, Vb + (j < n ? j * a.av.sl : 0), j < n && inv);
+        tc::copy16(to + 2 * u * RW_T, Kb + (j < n ? j * a.ak.sl : 0), j < n && inq);
+        tc::copy16(to + (2 * u + 1) * RW_T, Vb + (j < n ? j * a.av.sl : 0), j < n && inv);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");

@@ -49,7 +49,6 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-
 // Every wait is bounded: after about a second without progress the waiter raises the abort
 // flag of its block, latches a TIMEOUT status for the host and returns false; the caller
 // leaves its loop, so the block still reaches its common exit (TMEM release).  The single
@@ -204,6 +203,11 @@ __device__ __forceinline__ void bulk_load(void* smem_dst, const void* gsrc, uint
                "l"(reinterpret_cast<uint64_t>(gsrc)), "r"(bytes), "r"(smem_u32(bar))
                : "memory");
 }
+// 16 bytes into shared memory by this thread's asynchronous copies, zeros where there is nothing to read (`from` is then not read).
+__device__ __forceinline__ void copy16(void* to, const void* from, bool some) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(some ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ void prefetch_tmap(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
 }

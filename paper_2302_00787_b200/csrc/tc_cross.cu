@@ -27,7 +27,7 @@ constexpr int CX_REGS_REST = 56, CX_REGS_ROWS = 224;                   // 384 th
 constexpr uint32_t CX_TMEM = 512;
 constexpr float CX_SLACK = 8.f;
 #ifndef CX_CUBIC
-#define CX_CUBIC 3
+#define CX_CUBIC 1
 #endif
 
 template <int D>
@@ -51,7 +51,8 @@ struct CxMs {
 };
 static_assert(sizeof(CxMs) <= 512, "misc block");
 
-template <int D>
+// MASK: some keys may be hidden anywhere, not only behind a sequence's end.
+template <int D, bool MASK>
 __global__ void __launch_bounds__(CX_T, 1)
 tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CrossArgs a,
                 __nv_bfloat16* __restrict__ Y, TensorAddr ay, float* __restrict__ lse, CrossPart part, int* __restrict__ status) {
@@ -170,10 +171,11 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       const __nv_bfloat16* Q = static_cast<const __nv_bfloat16*>(a.Q) + b * a.aq.sb;
       for (int i = threadIdx.x; i < rows * CH; i += 256) {
         const int rr = i / CH, ch = i % CH, r = r0 + rr;
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (r < R && ch * 8 < a.d) x = *reinterpret_cast<const uint4*>(Q + (int64_t)(hk * a.g + r / a.Lq) * a.aq.sh + (int64_t)(r % a.Lq) * a.aq.sl + ch * 8);
-        *reinterpret_cast<uint4*>(sm + Sm::Q + (rr >> 7) * Sm::QT + (ch >> 3) * TILE_BYTES + sw128_offset(rr & 127, (ch & 7) * 8)) = x;
+        const bool some = r < R && ch * 8 < a.d;
+        copy16(sm + Sm::Q + (rr >> 7) * Sm::QT + (ch >> 3) * TILE_BYTES + sw128_offset(rr & 127, (ch & 7) * 8),
+               Q + (some ? (int64_t)(hk * a.g + r / a.Lq) * a.aq.sh + (int64_t)(r % a.Lq) * a.aq.sl + ch * 8 : 0), some);
       }
+      copies_done();
       fence_proxy_async_smem();
       mbar_arrive_warp(&misc->q_ready, lane);
     }
@@ -185,13 +187,23 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     float m = -INFINITY;
     uint32_t l[2] = {0u, 0u};
     bool ok = true;
+    // The mask's bytes of a tile are asked for one tile ahead.
+    uint8_t look[KT / 32];
+    auto peek = [&](int t) {
+#pragma unroll
+      for (int q = 0; q < KT / 32; q++) {
+        const int j = (t0 + t) * KT + q * 32 + lane;
+        look[q] = j < n ? a.key_mask[b * a.mask_stride + j] : 1;
+      }
+    };
+    if (MASK && mine > 0) peek(both ? 0 : w);
     for (int i = 0; i < mine; i++) {
       const int t = both ? i : 2 * i + w, j0 = (t0 + t) * KT;
       uint32_t seen[KT / 32];
-      const bool some = a.key_mask != nullptr || j0 + KT > n;           // some key of the tile may be hidden
+      const bool some = MASK || j0 + KT > n;           // some key of the tile may be hidden
       if (some) {
 #pragma unroll
-        for (int q = 0; q < KT / 32; q++) seen[q] = __ballot_sync(0xffffffffu, cross_seen(a, b, j0 + q * 32 + lane, n));
+        for (int q = 0; q < KT / 32; q++) seen[q] = __ballot_sync(0xffffffffu, j0 + q * 32 + lane < n && (!MASK || look[q] != 0));
         if (!both || w == 0) {
           // what a hidden key's V holds may be anything: zeros in its place, thread = key (one warpgroup does it for both: the
           // other's product is issued behind its own)
@@ -207,6 +219,7 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       ok = ok && __all_sync(0xffffffffu, mbar_wait(&misc->s_full[w], i & 1, abortp, status, false));
       if (!ok) break;
       tcgen05_fence_after();
+      if (MASK && i + 1 < mine) peek(both ? i + 1 : 2 * i + 2 + w);
       if (!idle) {
         uint32_t s[KT];
 #pragma unroll
@@ -369,9 +382,10 @@ template <int D>
 int launch(fsharp_ctx* ctx, const CUtensorMap& tmK, const CUtensorMap& tmV, const CrossArgs& a, void* Y, TensorAddr ay, float* lse, CrossPart part) {
   const int64_t gx = ((int64_t)a.g * a.Lq + 255) / 256 * part.pieces;
   if (gx > 0x7fffffff) return FSHARP_E_SHAPE;
-  FS_CUDA_OK(fs_allow_smem(tc_cross_kernel<D>));
+  const auto kernel = a.key_mask ? tc_cross_kernel<D, true> : tc_cross_kernel<D, false>;
+  FS_CUDA_OK(fs_allow_smem(kernel));
   FS_TIME_BEGIN(ctx, FS_K_TC_CROSS);
-  tc_cross_kernel<D><<<dim3((unsigned)gx, (unsigned)(a.B * a.Hk)), CX_T, CxSm<D>::TOTAL + 1024, ctx->stream>>>(
+  kernel<<<dim3((unsigned)gx, (unsigned)(a.B * a.Hk)), CX_T, CxSm<D>::TOTAL + 1024, ctx->stream>>>(
       tmK, tmV, a, static_cast<__nv_bfloat16*>(Y), ay, lse, part, ctx->d_status);
   FS_TIME_END(ctx);
   FS_LAUNCH_CHECK(ctx);

@@ -1,13 +1,12 @@
 // Gradients of the exact cross attention of bf16 tensors on the tensor cores, from P = 2^(x - lse) made again:
-//   dkv   per 128 keys, over the rows in tiles of 64:  S^T = K Q^T, dP^T = V dY^T;  dV += P^T dY, dK += dS^T Q
-//   dq    per 256 rows (128 per warpgroup), over the keys in tiles of 64:  S = Q K^T, dP = dY V^T;  dQ += dS K
+//   dkv   per 128 keys, over the rows in tiles:  S^T = K Q^T, dP^T = V dY^T;  dV += P^T dY, dK += dS^T Q
+//   dq    per 256 rows, over the keys in tiles:  S = Q K^T, dP = dY V^T;  dQ += dS K
 // with dS = P (dP - D); the scores' factor is applied to the sums at the end.  P and dS, rounded to bf16, are operands in tensor
-// memory, where the scores and dP were; thread = key (dkv) or row (dq).  Two kernels that both make P instead of one that adds
-// dQ up in memory with atomics: sums keep a fixed order, and the exponentials, made twice, hide under the products.
-// Two warpgroups take the tiles in turn (dkv), so that one's products run while the other is at its exponentials; in dq each has
-// rows of its own and they share every K and V tile (up to 128 rows: tiles in turn, two partial dQ that meet at the end).
-// Bound: the tensor pipe (four products of 128 x 64 x d per tile in dkv, three in dq; with N = 64 the two that read both operands
-// from shared memory are bound by its 128 bytes per clock) and the exponentials beside it.
+// memory; thread = key (dkv) or row (dq).  Two kernels that both make P instead of one that adds dQ up in memory with atomics: sums
+// keep a fixed order.
+// Bound: the tensor pipe and, beside it, shared memory: a product with both operands there moves 128 bytes per clock where N = 128 and 192
+// where N = 64, its tiles' copies come on top; then the exponentials and the way from a product's end to the warps that wait for it
+// (without the warpgroups' arithmetic the two kernels of 2 x 16 heads on 8, 2048 x 4096, d = 128, take 219 us of 279 and 264 of 278).
 #include "cross.cuh"
 #include "tc_common.cuh"
 #include "tc_cross.cuh"
@@ -22,38 +21,68 @@ int fs_tc_cross_map(CUtensorMap* map, const void* base, TensorAddr t, int B, int
 namespace {
 
 constexpr int CG_WARPS = 8, CGW_TMA = 8, CGW_MMA = 9, CG_T = 384;      // (warps 10, 11 only hand their registers over)
-constexpr int HALF = 64;                                                // rows (dkv) or keys (dq) of a walked tile
+constexpr int CG_REGS_REST = 56, CG_REGS_ROWS = 224;                   // 384 threads x 168 at launch = 128 x 56 + 256 x 224
+constexpr int CG_REGS_REST2 = 32, CG_REGS_ROWS2 = 104;                 // two blocks on an SM: 384 x 80 at launch = 128 x 32 + 256 x 104
+constexpr int HALF = 64;                                                // keys of a tile in dq
 constexpr uint32_t HALF_BYTES = 8192;                                   // 64 rows x 128 bytes
-constexpr uint32_t CG_TMEM = 512, CG_SUM = 256;                         // two pairs (S, dP) of 64 columns each, then the sums
+constexpr uint32_t CG_DQ_TMEM = 512, CG_DQ_SUM = 256;                   // dq: two pairs (S, dP) of 64 columns each, then the two dQ
 
-// The exponentials of 64 columns, those of every other four by the cubic, and dS; packed into the places of the first 32 registers.
-// (nl, nd): -lse log2(e) and -D of the columns (dkv).
+// Two exponentials, by the special-function unit or by the cubic (one in four).
 __device__ __forceinline__ void exps2(uint32_t& x, uint32_t& y, bool cubic) {
   if (cubic) exp2_poly2(x, y);
   else { x = __float_as_uint(ex2(__uint_as_float(x))); y = __float_as_uint(ex2(__uint_as_float(y))); }
 }
 
+// 16 values of a row, all of its warp's lanes together: to fp32 sums of a piece, or rounded to the gradient.
+__device__ __forceinline__ void store_row(bool on, const float (&x)[16], float* part, __nv_bfloat16* out) {
+  if (on && part) {
+#pragma unroll
+    for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(part + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+  } else if (on) {
+#pragma unroll
+    for (int k = 0; k < 16; k += 8)
+      *reinterpret_cast<uint4*>(out + k) = make_uint4(pack_bf16(x[k], x[k + 1]), pack_bf16(x[k + 2], x[k + 3]), pack_bf16(x[k + 4], x[k + 5]), pack_bf16(x[k + 6], x[k + 7]));
+  }
+  __syncwarp();
+}
+
 // ------------------------------------------------------------------------------------------ dK, dV
+// The products of a tile are issued so that what the warpgroups make is wanted two products later: dV, next S^T, dK, next dP^T; each
+// warpgroup has half of a tile's rows.  At d = 64 two blocks on an SM, tiles of 64 rows, hide each other's starts and ends (16 x 12 x 512 x
+// 1500: 152 us with one block, 118).
+// Columns of tensor memory: S^T and dP^T of the tile (T rows: T columns each; P^T and dS^T, two to a column, lie over them: the first
+// warpgroup's T / 2 rows at the front, the second's from column T / 2 on, so that neither writes what the other has yet to read), dV, dK.
 template <int D>
 struct KvSm {
-  static constexpr int PANELS = D / 64, NS = D == 64 ? 6 : 4;
-  static constexpr uint32_t K = 0, V = PANELS * TILE_BYTES, RING = 2 * PANELS * TILE_BYTES, SLOT = PANELS * HALF_BYTES, STAGE = 2 * SLOT;
-  static constexpr uint32_t STAT = RING + NS * STAGE, MISC = STAT + NS * 512, TOTAL = MISC + 512;
-  static_assert(TOTAL + 1024 <= 232448, "shared memory budget");
+  static constexpr int T = D == 64 ? 64 : 128, BLOCKS = D == 64 ? 2 : 1, PANELS = D / 64, NS = D == 64 ? 4 : 2;      // NS: tiles of Q and of dY in flight
+  static constexpr uint32_t PANEL = T * 128, BIG = PANELS * TILE_BYTES, TILE_D = PANELS * PANEL, K = 0, V = BIG, Q = 2 * BIG, G = Q + NS * TILE_D, STAT = G + NS * TILE_D;
+  static constexpr uint32_t MISC = STAT + NS * 8 * T, TOTAL = MISC + 512;
+  static constexpr uint32_t S = 0, P = T, DV = 2 * T, DK = 2 * T + D, COLUMNS = BLOCKS == 2 ? 256 : 512;
+  static_assert(BLOCKS * (TOTAL + 2048) <= 233472, "shared memory budget");
+  static_assert(DK + D <= COLUMNS, "tensor memory");
 };
 struct KvMs {
-  uint64_t full[8], empty[8], sp_full[2], ready[2], kv_full, done;
+  uint64_t q_full[4], q_empty[4], g_full[4], g_empty[4], s_full, p_ready, dp_full, ds_ready, kv_full, done;
   uint32_t tmem_base;
   int abort_flag;
 };
 static_assert(sizeof(KvMs) <= 512, "misc block");
 
+// A = P^T or dS^T [128 x T] in tensor memory (its two halves T / 2 columns apart) times the tile's T rows in shared memory
+template <int T>
+__device__ __forceinline__ void issue_halves(uint32_t d_tmem, uint32_t a_tmem, Desc b, uint32_t idesc, uint32_t accumulate) {
+#pragma unroll
+  for (int k = 0; k < T / 16; k++)
+    mma_bf16_ta_lh(d_tmem, a_tmem + k / (T / 32) * (T / 2) + k % (T / 32) * 8, b.lo + k * (2048 / 16), b.hi, idesc, k > 0 ? 1u : accumulate);
+}
+
 template <int D>
-__global__ void __launch_bounds__(CG_T, 1)
+__global__ void __launch_bounds__(CG_T, KvSm<D>::BLOCKS)
 tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmG, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CrossArgs a, const __grid_constant__ CrossGrad gr,
                     int* __restrict__ status) {
   using Sm = KvSm<D>;
+  constexpr int T = Sm::T;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   KvMs* misc = reinterpret_cast<KvMs*>(sm + Sm::MISC);
@@ -62,20 +91,23 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   const int unit = blockIdx.y, piece = blockIdx.x % gr.kv_pieces, j0 = (int)(blockIdx.x / gr.kv_pieces) * TILE;
   const int b = unit / a.Hk, hk = unit % a.Hk, n = cross_keys(a, b);
   // row tiles: those of the first query head of the group, of the second, ...
-  const int per = (a.Lq + HALF - 1) / HALF;
+  const int per = (a.Lq + T - 1) / T;
   const int64_t tiles = j0 < n ? (int64_t)a.g * per : 0;
   const int t0 = (int)(tiles * piece / gr.kv_pieces), items = (int)(tiles * (piece + 1) / gr.kv_pieces) - t0;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < Sm::NS; i++) { mbar_init(&misc->full[i], 1); mbar_init(&misc->empty[i], 1); }
-    for (int w = 0; w < 2; w++) { mbar_init(&misc->sp_full[w], 1); mbar_init(&misc->ready[w], 4); }
+    for (int i = 0; i < Sm::NS; i++) { mbar_init(&misc->q_full[i], 1); mbar_init(&misc->q_empty[i], 1); mbar_init(&misc->g_full[i], 1); mbar_init(&misc->g_empty[i], 1); }
+    mbar_init(&misc->s_full, 1);
+    mbar_init(&misc->dp_full, 1);
+    mbar_init(&misc->p_ready, CG_WARPS);
+    mbar_init(&misc->ds_ready, CG_WARPS);
     mbar_init(&misc->kv_full, 1);
     mbar_init(&misc->done, 1);
     misc->abort_flag = 0;
     fence_barrier_init();
   }
   if (warp == CGW_MMA) {
-    tmem_alloc(&misc->tmem_base, CG_TMEM);
+    tmem_alloc(&misc->tmem_base, Sm::COLUMNS);
     tmem_relinquish();
   }
   tcgen05_fence_before();
@@ -84,7 +116,7 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   const uint32_t tmem = misc->tmem_base;
   const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;
 
-  if (warp >= CG_WARPS) regs_release<REGS_PRODUCER>();
+  if (warp >= CG_WARPS) regs_release<(Sm::BLOCKS == 2 ? CG_REGS_REST2 : CG_REGS_REST)>();
   if (warp == CGW_TMA) {
     if (lane == 0 && items > 0) {
       prefetch_tmap(&tmQ); prefetch_tmap(&tmG); prefetch_tmap(&tmK); prefetch_tmap(&tmV);
@@ -94,109 +126,153 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       int i = 0;
       for (; i < items; i++) {
         const int s = i % Sm::NS, h = hk * a.g + (t0 + i) / per, t = (t0 + i) % per;
-        if (!mbar_wait(&misc->empty[s], ((i / Sm::NS) & 1) ^ 1, abortp, status)) break;
-        uint8_t* base = sm + Sm::RING + s * Sm::STAGE;
-        mbar_expect_tx(&misc->full[s], (kp + vp) * HALF_BYTES + 512);
-        for (int p = 0; p < kp; p++) tma_load_4d(base + p * HALF_BYTES, &tmQ, &misc->full[s], p * 64, t * HALF, a.aq.sh ? h : 0, a.aq.sb ? b : 0);
+        const uint32_t parity = ((i / Sm::NS) & 1) ^ 1;
+        if (!mbar_wait(&misc->q_empty[s], parity, abortp, status)) break;
+        mbar_expect_tx(&misc->q_full[s], kp * Sm::PANEL + 8 * T);
+        for (int p = 0; p < kp; p++)
+          tma_load_4d(sm + Sm::Q + s * Sm::TILE_D + p * Sm::PANEL, &tmQ, &misc->q_full[s], p * 64, t * T, a.aq.sh ? h : 0, a.aq.sb ? b : 0);
+        const float* st = gr.stat + ((int64_t)b * a.H + h) * cross_stat_floats(a.Lq) + (int64_t)(t * T / 128) * 256 + t * T % 128;
+        bulk_load(sm + Sm::STAT + s * 8 * T, st, 4 * T, &misc->q_full[s]);
+        bulk_load(sm + Sm::STAT + s * 8 * T + 4 * T, st + 128, 4 * T, &misc->q_full[s]);
+        // (dY of a tile is done with before its Q is: its place is free by now, or the block has given up)
+        if (!mbar_wait(&misc->g_empty[s], parity, abortp, status)) { mbar_wait(&misc->q_full[s], (i / Sm::NS) & 1, abortp, status, false); break; }
+        mbar_expect_tx(&misc->g_full[s], vp * Sm::PANEL);
         for (int p = 0; p < vp; p++)
-          tma_load_4d(base + Sm::SLOT + p * HALF_BYTES, &tmG, &misc->full[s], p * 64, t * HALF, gr.ady.sh ? h : 0, gr.ady.sb ? b : 0);
-        bulk_load(sm + Sm::STAT + s * 512, gr.stat + ((int64_t)b * a.H + h) * cross_stat_floats(a.Lq) + (int64_t)t * 128, 512, &misc->full[s]);
+          tma_load_4d(sm + Sm::G + s * Sm::TILE_D + p * Sm::PANEL, &tmG, &misc->g_full[s], p * 64, t * T, gr.ady.sh ? h : 0, gr.ady.sb ? b : 0);
       }
       // nothing of this block may still be in flight when it exits: no copy, and no arrival of a product's completion
       mbar_wait(&misc->kv_full, 0, abortp, status, false);
       for (int k = max(0, i - Sm::NS); k < i; k++) {
-        mbar_wait(&misc->full[k % Sm::NS], (k / Sm::NS) & 1, abortp, status, false);
-        mbar_wait(&misc->empty[k % Sm::NS], (k / Sm::NS) & 1, abortp, status);
+        const uint32_t parity = (k / Sm::NS) & 1;
+        mbar_wait(&misc->q_full[k % Sm::NS], parity, abortp, status, false);
+        mbar_wait(&misc->g_full[k % Sm::NS], parity, abortp, status, false);
+        mbar_wait(&misc->q_empty[k % Sm::NS], parity, abortp, status);
+        mbar_wait(&misc->g_empty[k % Sm::NS], parity, abortp, status);
       }
     }
   } else if (warp == CGW_MMA) {
-    constexpr uint32_t ID_S = idesc_bf16(128, HALF, 0, 0);
+    // dV of a tile, S^T of the next, dK, dP^T of the next: each needs what the warpgroups made during the two before it.
+    constexpr uint32_t ID_S = idesc_bf16(128, T, 0, 0);
     const uint32_t ID_V = idesc_bf16(128, a.dv, 0, 1), ID_K = idesc_bf16(128, a.d, 0, 1);
-    const uint32_t sR = smem_u32(sm + Sm::RING);
+    const uint32_t sQ = smem_u32(sm + Sm::Q), sG = smem_u32(sm + Sm::G);
     const Desc k0 = smem_desc(smem_u32(sm + Sm::K), 16, 1024, SWZ_128B), v0 = smem_desc(smem_u32(sm + Sm::V), 16, 1024, SWZ_128B);
-    const Desc q0 = smem_desc(sR, 16, 1024, SWZ_128B), qt = smem_desc(sR, HALF_BYTES, 1024, SWZ_128B);      // dY: a slot behind Q
+    const Desc q0 = smem_desc(sQ, 16, 1024, SWZ_128B), g0 = smem_desc(sG, 16, 1024, SWZ_128B);
+    // the same tiles with their rows as the contraction: panels of 64 columns, 16 rows of 128 bytes per step
+    const Desc qt = smem_desc(sQ, Sm::PANEL, 1024, SWZ_128B), gt = smem_desc(sG, Sm::PANEL, 1024, SWZ_128B);
     const int ks = a.d / 16, vs = a.dv / 16;
     const bool leader = elect_one();
     auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, abortp, status); };
-    int slot = 0, phase = 0, done = 0;                 // the next tile's stage; the stage of the tile whose sums come next
-    auto issue_sp = [&](int w) {                       // S^T and dP^T of the next tile, which is warpgroup w's
-      if (!wait(&misc->full[slot], phase)) return false;
+    auto issue_s = [&](int i) {
+      const int s = i % Sm::NS;
+      if (!wait(&misc->q_full[s], (i / Sm::NS) & 1)) return false;
       tcgen05_fence_after();
       if (leader) {
         Desc q = q0;
-        q.lo += slot * (Sm::STAGE / 16);
-        issue_rows<D / 16, TILE_BYTES, HALF_BYTES>(tmem + w * 128, k0, q, ID_S, ks);
-        q.lo += Sm::SLOT / 16;
-        issue_rows<D / 16, TILE_BYTES, HALF_BYTES>(tmem + w * 128 + 64, v0, q, ID_S, vs);
-        mma_commit(&misc->sp_full[w]);
+        q.lo += s * (Sm::TILE_D / 16);
+        issue_rows<D / 16, TILE_BYTES, Sm::PANEL>(tmem + Sm::S, k0, q, ID_S, ks);
+        mma_commit(&misc->s_full);
       }
       __syncwarp();
-      if (++slot == Sm::NS) { slot = 0; phase ^= 1; }
       return true;
     };
-    bool ok = items > 0 && wait(&misc->kv_full, 0) && issue_sp(0) && (items < 2 || issue_sp(1));
-    auto item = [&](int i, int w) {
-      if (!wait(&misc->ready[w], (i >> 1) & 1)) return false;
+    auto issue_dp = [&](int i) {
+      const int s = i % Sm::NS;
+      if (!wait(&misc->g_full[s], (i / Sm::NS) & 1)) return false;
       tcgen05_fence_after();
       if (leader) {
-        // Q and dY again, now with their rows as the contraction: panels of 64 columns, 16 rows of 128 bytes per step
+        Desc g = g0;
+        g.lo += s * (Sm::TILE_D / 16);
+        issue_rows<D / 16, TILE_BYTES, Sm::PANEL>(tmem + Sm::P, v0, g, ID_S, vs);
+        mma_commit(&misc->dp_full);
+      }
+      __syncwarp();
+      return true;
+    };
+    bool ok = items > 0 && wait(&misc->kv_full, 0) && issue_s(0) && issue_dp(0);
+    for (int i = 0; i < items && ok; i++) {
+      const int s = i % Sm::NS;
+      if (!(ok = wait(&misc->p_ready, i & 1))) break;
+      tcgen05_fence_after();
+      if (leader) {
+        Desc g = gt;
+        g.lo += s * (Sm::TILE_D / 16);
+        issue_halves<T>(tmem + Sm::DV, tmem + Sm::S, g, ID_V, i > 0);
+        mma_commit(&misc->g_empty[s]);
+      }
+      __syncwarp();
+      if (i + 1 < items && !(ok = issue_s(i + 1))) break;
+      if (!(ok = wait(&misc->ds_ready, i & 1))) break;
+      tcgen05_fence_after();
+      if (leader) {
         Desc q = qt;
-        q.lo += done * (Sm::STAGE / 16);
-        issue_cols<4>(tmem + CG_SUM + D, tmem + w * 128 + 64, q, ID_K, i > 0);
-        q.lo += Sm::SLOT / 16;
-        issue_cols<4>(tmem + CG_SUM, tmem + w * 128, q, ID_V, i > 0);
-        mma_commit(&misc->empty[done]);
+        q.lo += s * (Sm::TILE_D / 16);
+        issue_halves<T>(tmem + Sm::DK, tmem + Sm::P, q, ID_K, i > 0);
+        mma_commit(&misc->q_empty[s]);
         if (i == items - 1) mma_commit(&misc->done);
       }
       __syncwarp();
-      if (++done == Sm::NS) done = 0;
-      return i + 2 >= items || issue_sp(w);
-    };
-    for (int i = 0; i < items && ok; i += 2) ok = item(i, 0) && (i + 1 >= items || item(i + 1, 1));
+      if (i + 1 < items) ok = issue_dp(i + 1);
+    }
   } else if (warp < CG_WARPS) {
-    regs_acquire<REGS_EPILOGUE>();
-    const int w = warp >> 2, row = (warp & 3) * 32 + lane;
-    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), tS = lanes + w * 128, tP = tS + 64;
+    regs_acquire<(Sm::BLOCKS == 2 ? CG_REGS_ROWS2 : CG_REGS_ROWS)>();
+    const int w = warp >> 2, row = (warp & 3) * 32 + lane;      // w: which half of the tile's rows
+    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), tS = lanes + Sm::S + w * (T / 2), tP = lanes + Sm::P + w * (T / 2);
     const float c = a.scale * FS_LOG2E;
     bool ok = true;
-    for (int i = w; i < items; i += 2) {
+    for (int i = 0; i < items; i++) {
       const int s = i % Sm::NS;
       // (what a hidden key holds, NaNs too, stays in its own row of S^T, dP^T and of the sums, and is dropped at the end)
-      ok = __all_sync(0xffffffffu, mbar_wait(&misc->sp_full[w], (i >> 1) & 1, abortp, status, false) &&
-                                       mbar_wait(&misc->full[s], (i / Sm::NS) & 1, abortp, status, false));
+      ok = __all_sync(0xffffffffu, mbar_wait(&misc->s_full, i & 1, abortp, status, false) &&
+                                       mbar_wait(&misc->q_full[s], (i / Sm::NS) & 1, abortp, status, false));
       if (!ok) break;
       tcgen05_fence_after();
-      const float* st = reinterpret_cast<const float*>(sm + Sm::STAT + s * 512);
-      uint32_t x[64], g[64];
+      const float* st = reinterpret_cast<const float*>(sm + Sm::STAT + s * 8 * T) + w * (T / 2);
+      uint32_t x[T / 2], g[T / 2];
 #pragma unroll
-      for (int q = 0; q < 4; q++) tmem_ld16(tS + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(x + 16 * q));
-#pragma unroll
-      for (int q = 0; q < 4; q++) tmem_ld16(tP + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(g + 16 * q));
+      for (int q = 0; q < T / 32; q++) tmem_ld16(tS + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(x + 16 * q));
       tmem_wait_ld();
 #pragma unroll
-      for (int q = 0; q < 64; q += 32) {
-        uint32_t o[16], u[16];
+      for (int q = 0; q < T / 2; q += 32) {
+        uint32_t o[16];
 #pragma unroll
         for (int k = 0; k < 32; k += 4) {
-          const float4 nl = *reinterpret_cast<const float4*>(st + q + k), nd = *reinterpret_cast<const float4*>(st + 64 + q + k);
-          uint32_t *xp = x + q + k, *gp = g + q + k;
+          const float4 nl = *reinterpret_cast<const float4*>(st + q + k);
+          uint32_t* xp = x + q + k;
           fma2v(xp[0], xp[1], c, nl.x, nl.y);
           fma2v(xp[2], xp[3], c, nl.z, nl.w);
           exps2(xp[0], xp[1], false);
-          exps2(xp[2], xp[3], true);
-          addmul2(gp[0], gp[1], nd.x, nd.y, xp[0], xp[1]);
-          addmul2(gp[2], gp[3], nd.z, nd.w, xp[2], xp[3]);
+          exps2(xp[2], xp[3], (k & 4) != 0);
           o[k / 2] = pack_bf16(__uint_as_float(xp[0]), __uint_as_float(xp[1]));
           o[k / 2 + 1] = pack_bf16(__uint_as_float(xp[2]), __uint_as_float(xp[3]));
+        }
+        tmem_st16(tS + q / 2, o);
+      }
+      tmem_wait_st();
+      tcgen05_fence_before();
+      mbar_arrive_warp(&misc->p_ready, lane);
+      ok = __all_sync(0xffffffffu, mbar_wait(&misc->dp_full, i & 1, abortp, status, false));
+      if (!ok) break;
+      tcgen05_fence_after();
+#pragma unroll
+      for (int q = 0; q < T / 32; q++) tmem_ld16(tP + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(g + 16 * q));
+      tmem_wait_ld();
+#pragma unroll
+      for (int q = 0; q < T / 2; q += 32) {
+        uint32_t u[16];
+#pragma unroll
+        for (int k = 0; k < 32; k += 4) {
+          const float4 nd = *reinterpret_cast<const float4*>(st + T + q + k);
+          uint32_t *xp = x + q + k, *gp = g + q + k;
+          addmul2(gp[0], gp[1], nd.x, nd.y, xp[0], xp[1]);
+          addmul2(gp[2], gp[3], nd.z, nd.w, xp[2], xp[3]);
           u[k / 2] = pack_bf16(__uint_as_float(gp[0]), __uint_as_float(gp[1]));
           u[k / 2 + 1] = pack_bf16(__uint_as_float(gp[2]), __uint_as_float(gp[3]));
         }
-        tmem_st16(tS + q / 2, o);
         tmem_st16(tP + q / 2, u);
       }
       tmem_wait_st();
       tcgen05_fence_before();
-      mbar_arrive_warp(&misc->ready[w], lane);
+      mbar_arrive_warp(&misc->ds_ready, lane);
     }
     if (ok && items > 0) ok = __all_sync(0xffffffffu, mbar_wait(&misc->done, 0, abortp, status, false));
     tcgen05_fence_after();
@@ -211,21 +287,13 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       for (int q = 0; q < width; q += 16) {
         uint32_t t[16] = {};
         if (items > 0) {
-          tmem_ld16(lanes + CG_SUM + w * D + q, t);
+          tmem_ld16(lanes + (w ? Sm::DK : Sm::DV) + q, t);
           tmem_wait_ld();
         }
         float x[16];
 #pragma unroll
         for (int k = 0; k < 16; k++) x[k] = on ? __uint_as_float(t[k]) * f : 0.f;
-        if (j < a.Lk && gr.pkv) {
-#pragma unroll
-          for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(part + q + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
-        } else if (j < a.Lk) {
-#pragma unroll
-          for (int k = 0; k < 16; k += 8)
-            *reinterpret_cast<uint4*>(out + q + k) = make_uint4(pack_bf16(x[k], x[k + 1]), pack_bf16(x[k + 2], x[k + 3]), pack_bf16(x[k + 4], x[k + 5]), pack_bf16(x[k + 6], x[k + 7]));
-        }
-        __syncwarp();
+        store_row(j < a.Lk, x, gr.pkv ? part + q : nullptr, out + q);
       }
     }
   }
@@ -233,11 +301,15 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   __syncthreads();
   if (warp == CGW_MMA) {
     tcgen05_fence_after();
-    tmem_dealloc(tmem, CG_TMEM);
+    tmem_dealloc(tmem, Sm::COLUMNS);
   }
 }
 
 // ------------------------------------------------------------------------------------------ dQ
+// Up to 256 rows of a unit per block, 128 per warpgroup, over the keys in tiles of 64; each warpgroup has S, dP (dS, two to a column, lies
+// over S) and dQ of its own, and they share every K and V tile (up to 128 rows: tiles in turn, two partial dQ that meet at the end).
+// (128 rows per block, both warpgroups on halves of its tiles: twice the copies, 278 us instead of 234 for 2 x 16 heads on 8,
+// 2048 x 4096, d = 128, the same 92 us for 16 x 12 x 512 x 1500, d = 64.)
 template <int D>
 struct DqSm {
   static constexpr int PANELS = D / 64, NS = D == 64 ? 6 : 3;
@@ -278,7 +350,7 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     fence_barrier_init();
   }
   if (warp == CGW_MMA) {
-    tmem_alloc(&misc->tmem_base, CG_TMEM);
+    tmem_alloc(&misc->tmem_base, CG_DQ_TMEM);
     tmem_relinquish();
   }
   tcgen05_fence_before();
@@ -287,7 +359,7 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   const uint32_t tmem = misc->tmem_base;
   const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;
 
-  if (warp >= CG_WARPS) regs_release<REGS_PRODUCER>();
+  if (warp >= CG_WARPS) regs_release<CG_REGS_REST>();
   if (warp == CGW_TMA) {
     if (lane == 0) {
       prefetch_tmap(&tmK); prefetch_tmap(&tmV);
@@ -344,7 +416,7 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       if (leader) {
         Desc k = kt;                                   // its keys as the contraction
         k.lo += done * (Sm::STAGE / 16);
-        issue_cols<4>(tmem + CG_SUM + w * 128, tmem + w * 128, k, ID_Q, i > 1);
+        issue_cols<4>(tmem + CG_DQ_SUM + w * 128, tmem + w * 128, k, ID_Q, i > 1);
         if (!both || w) mma_commit(&misc->empty[done]);
         if (i + 2 >= items) mma_commit(&misc->done[w]);
       }
@@ -354,7 +426,7 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     };
     for (int i = 0; i < items && ok; i += 2) ok = item(i, 0) && (i + 1 >= items || item(i + 1, 1));
   } else if (warp < CG_WARPS) {
-    regs_acquire<REGS_EPILOGUE>();
+    regs_acquire<CG_REGS_ROWS>();
     const int w = warp >> 2, row = (warp & 3) * 32 + lane;
     {
       // the block's rows of Q and dY into shared memory, rows and columns that there are none of as zeros
@@ -364,14 +436,15 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const int which = i >= rows * CH, k = i - which * rows * CH, rr = k / CH, ch = k % CH, r = r0 + rr;
         const TensorAddr t = which ? gr.ady : a.aq;
         const __nv_bfloat16* X = static_cast<const __nv_bfloat16*>(which ? gr.dY : a.Q) + b * t.sb;
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (r < R && ch * 8 < (which ? a.dv : a.d)) x = *reinterpret_cast<const uint4*>(X + (int64_t)(hk * a.g + r / a.Lq) * t.sh + (int64_t)(r % a.Lq) * t.sl + ch * 8);
-        *reinterpret_cast<uint4*>(sm + (which ? Sm::G : Sm::Q) + (rr >> 7) * Sm::BIG + (ch >> 3) * TILE_BYTES + sw128_offset(rr & 127, (ch & 7) * 8)) = x;
+        const bool some = r < R && ch * 8 < (which ? a.dv : a.d);
+        copy16(sm + (which ? Sm::G : Sm::Q) + (rr >> 7) * Sm::BIG + (ch >> 3) * TILE_BYTES + sw128_offset(rr & 127, (ch & 7) * 8),
+               X + (some ? (int64_t)(hk * a.g + r / a.Lq) * t.sh + (int64_t)(r % a.Lq) * t.sl + ch * 8 : 0), some);
       }
+      copies_done();
       fence_proxy_async_smem();
       mbar_arrive_warp(&misc->q_ready, lane);
     }
-    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), tS = lanes + w * 128, tP = tS + 64, tQ = lanes + CG_SUM + w * 128;
+    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), tS = lanes + w * 128, tP = tS + 64, tQ = lanes + CG_DQ_SUM + w * 128;
     const int first = r0 + (both ? w * TILE : 0), r = first + row;
     const bool idle = first + (warp & 3) * 32 >= R;
     const int mine = both ? nt : (nt + 1 - w) / 2;
@@ -411,7 +484,7 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           fma2(x[k], x[k + 1], c, st.x);
           fma2(x[k + 2], x[k + 3], c, st.x);
           exps2(x[k], x[k + 1], false);
-          exps2(x[k + 2], x[k + 3], true);
+          exps2(x[k + 2], x[k + 3], (k & 4) != 0);
           addmul2(g[k], g[k + 1], st.y, st.y, x[k], x[k + 1]);
           addmul2(g[k + 2], g[k + 3], st.y, st.y, x[k + 2], x[k + 3]);
         }
@@ -463,15 +536,7 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         float x[16];
 #pragma unroll
         for (int k = 0; k < 16; k++) x[k] = a.scale * (__uint_as_float(o[k]) + (both ? 0.f : xo[row * (D + 1) + q + k]));
-        if (r < R && gr.pq) {
-#pragma unroll
-          for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(part + q + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
-        } else if (r < R) {
-#pragma unroll
-          for (int k = 0; k < 16; k += 8)
-            *reinterpret_cast<uint4*>(out + q + k) = make_uint4(pack_bf16(x[k], x[k + 1]), pack_bf16(x[k + 2], x[k + 3]), pack_bf16(x[k + 4], x[k + 5]), pack_bf16(x[k + 6], x[k + 7]));
-        }
-        __syncwarp();
+        store_row(r < R, x, gr.pq ? part + q : nullptr, out + q);
       }
     }
   }
@@ -479,7 +544,7 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   __syncthreads();
   if (warp == CGW_MMA) {
     tcgen05_fence_after();
-    tmem_dealloc(tmem, CG_TMEM);
+    tmem_dealloc(tmem, CG_DQ_TMEM);
   }
 }
 
@@ -487,13 +552,13 @@ template <int D>
 int launch(fsharp_ctx* ctx, const CrossArgs& a, const CrossGrad& gr) {
   const int64_t gk = ((int64_t)a.Lk + TILE - 1) / TILE * gr.kv_pieces, gq = ((int64_t)a.g * a.Lq + 255) / 256 * gr.q_pieces;
   if (gk > 0x7fffffff || gq > 0x7fffffff) return FSHARP_E_SHAPE;
-  CUtensorMap tmQ, tmG, tmK, tmV, tmK64, tmV64;
-  FS_TRY(fs_tc_cross_map(&tmQ, a.Q, a.aq, a.B, a.H, a.Lq, a.d, HALF));
-  FS_TRY(fs_tc_cross_map(&tmG, gr.dY, gr.ady, a.B, a.H, a.Lq, a.dv, HALF));
+  CUtensorMap tmQ, tmG, tmK, tmV, tmKt, tmVt;
+  FS_TRY(fs_tc_cross_map(&tmQ, a.Q, a.aq, a.B, a.H, a.Lq, a.d, KvSm<D>::T));
+  FS_TRY(fs_tc_cross_map(&tmG, gr.dY, gr.ady, a.B, a.H, a.Lq, a.dv, KvSm<D>::T));
   FS_TRY(fs_tc_cross_map(&tmK, a.K, a.ak, a.B, a.Hk, a.Lk, a.d, TILE));
   FS_TRY(fs_tc_cross_map(&tmV, a.V, a.av, a.B, a.Hk, a.Lk, a.dv, TILE));
-  FS_TRY(fs_tc_cross_map(&tmK64, a.K, a.ak, a.B, a.Hk, a.Lk, a.d, HALF));
-  FS_TRY(fs_tc_cross_map(&tmV64, a.V, a.av, a.B, a.Hk, a.Lk, a.dv, HALF));
+  FS_TRY(fs_tc_cross_map(&tmKt, a.K, a.ak, a.B, a.Hk, a.Lk, a.d, HALF));
+  FS_TRY(fs_tc_cross_map(&tmVt, a.V, a.av, a.B, a.Hk, a.Lk, a.dv, HALF));
   FS_CUDA_OK(fs_allow_smem(tc_cross_dkv_kernel<D>));
   FS_CUDA_OK(fs_allow_smem(tc_cross_dq_kernel<D>));
   FS_TIME_BEGIN(ctx, FS_K_TC_CROSS_DKV);
@@ -501,16 +566,16 @@ int launch(fsharp_ctx* ctx, const CrossArgs& a, const CrossGrad& gr) {
   FS_TIME_END(ctx);
   FS_LAUNCH_CHECK(ctx);
   FS_TIME_BEGIN(ctx, FS_K_TC_CROSS_DQ);
-  tc_cross_dq_kernel<D><<<dim3((unsigned)gq, (unsigned)(a.B * a.Hk)), CG_T, DqSm<D>::TOTAL + 1024, ctx->stream>>>(tmK64, tmV64, a, gr, ctx->d_status);
+  tc_cross_dq_kernel<D><<<dim3((unsigned)gq, (unsigned)(a.B * a.Hk)), CG_T, DqSm<D>::TOTAL + 1024, ctx->stream>>>(tmKt, tmVt, a, gr, ctx->d_status);
   FS_TIME_END(ctx);
   FS_LAUNCH_CHECK(ctx);
   return FSHARP_OK;
 }
 
-// Pieces that bring `blocks` blocks up to one per SM, each with four tiles at least.
+// Pieces that bring `blocks` blocks up to one per SM, each with two tiles at least.
 int pieces_for(const fsharp_ctx* ctx, int64_t blocks, int64_t tiles) {
   int64_t p = ctx->sm_count / blocks;
-  if (p > tiles / 4) p = tiles / 4;
+  if (p > tiles / 2) p = tiles / 2;
   if (p > 64) p = 64;
   return p < 1 ? 1 : (int)p;
 }
@@ -518,9 +583,9 @@ int pieces_for(const fsharp_ctx* ctx, int64_t blocks, int64_t tiles) {
 }  // namespace
 
 void fs_tc_cross_grad_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int* kv_pieces, int* q_pieces) {
-  const int64_t g = dm->H / dm->Hk, units = (int64_t)dm->B * dm->Hk;
-  *kv_pieces = pieces_for(ctx, units * (((int64_t)dm->Lk + TILE - 1) / TILE), g * (((int64_t)dm->Lq + HALF - 1) / HALF));
-  *q_pieces = pieces_for(ctx, units * ((g * dm->Lq + 255) / 256), ((int64_t)dm->Lk + HALF - 1) / HALF);
+  const int64_t g = dm->H / dm->Hk, units = (int64_t)dm->B * dm->Hk, keys = ((int64_t)dm->Lk + TILE - 1) / TILE;
+  *kv_pieces = pieces_for(ctx, units * keys, g * (((int64_t)dm->Lq + TILE - 1) / TILE));
+  *q_pieces = pieces_for(ctx, units * ((g * dm->Lq + 255) / 256), keys);
 }
 
 int fs_tc_cross_grad(fsharp_ctx* ctx, const CrossArgs& a, const CrossGrad& gr) {
