@@ -52,7 +52,7 @@ enum {
   FS_K_PREFIX, FS_K_SCORES, FS_K_OUT, FS_K_PAIRS, FS_K_PAIRVAR_PREP, FS_K_PAIRVAR,
   FS_K_TC_KV, FS_K_TC_OUT, FS_K_TC_CAUSAL, FS_K_TC_STATS, FS_K_TC_ROWTERM, FS_K_TC_FEAT, FS_K_TC_KV128, FS_K_TC_OUT128,
   FS_K_PAIR_IMAGES, FS_K_W3, FS_K_BWD_STATE, FS_K_BWD_NUMDEN, FS_K_BWD_DFEAT, FS_K_BWD_DX, FS_K_BWD_DV, FS_K_TC_MERGE, FS_K_ROTATE,
-  FS_K_CROSS_ROWS, FS_K_CROSS_FMA, FS_K_CROSS_JOIN, FS_K_CROSS_DELTA, FS_K_CROSS_DKV, FS_K_CROSS_DQ, FS_K_CROSS_SUM,
+  FS_K_CROSS_ROWS, FS_K_CROSS_FMA, FS_K_CROSS_JOIN, FS_K_CROSS_DELTA, FS_K_CROSS_DKV, FS_K_CROSS_DQ, FS_K_CROSS_SUM, FS_K_CROSS_SPLIT,
   FS_K_TC_CROSS, FS_K_TC_CROSS_DKV, FS_K_TC_CROSS_DQ,
   FS_K_COUNT
 };

@@ -90,7 +90,7 @@ int check(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype) {
   if (dm->Hk && (int64_t)(dm->H / dm->Hk) * dm->Lq > 0x7ffffe00) return FSHARP_E_SHAPE;
   if (dm->Lk > 0x7ffffe00) return FSHARP_E_SHAPE;
   if (dtype != FSHARP_F32 && dtype != FSHARP_BF16) return FSHARP_E_DTYPE;
-  if (ctx->impl == FSHARP_IMPL_TENSOR && dtype != FSHARP_BF16) return FSHARP_E_SHAPE;
+  if (ctx->impl == FSHARP_IMPL_TENSOR && dtype != FSHARP_BF16 && (dm->d > 64 || dm->dv > 64)) return FSHARP_E_SHAPE;
   return FSHARP_OK;
 }
 
@@ -109,23 +109,36 @@ int check_tokens(const void* p, int dtype, const int64_t s[3], int L) {
   return L > 1 && s[2] == 0 && (s[0] != 0 || s[1] != 0) ? FSHARP_E_SHAPE : FSHARP_OK;
 }
 
-enum Kind { ROWS, FMA, TC };
+enum Kind { ROWS, FMA, TC, TC32 };
 struct Plan {
   Kind kind;
   int pieces;
   bool join;                   // the pieces meet in scratch
   int64_t o_floats, ml;        // partial results
+  int64_t parts;               // bf16 parts of fp32 operands
 };
+
+// Rows of a unit up to which fp32 takes the multiply-add tiles of 16 rows.
+constexpr int FMA_MOST_ROWS = 16;
+// fp32 on the tensor cores: heads that leave room for three parts of every operand in shared memory.
+bool parts_fit(const fsharp_cross_dims* dm) { return dm->d <= 64 && dm->dv <= 64; }
 
 Plan plan_forward(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype) {
   Plan p = {};
   const int64_t R = (int64_t)dm->H / dm->Hk * dm->Lq, units = (int64_t)dm->B * dm->Hk;
-  if (ctx->impl == FSHARP_IMPL_TENSOR) p.kind = TC;
+  const bool bf16 = dtype == FSHARP_BF16;
+  if (ctx->impl == FSHARP_IMPL_TENSOR) p.kind = bf16 ? TC : TC32;
   else if (R <= fs_cross_rows_most(dtype)) p.kind = ROWS;
-  else p.kind = dtype == FSHARP_BF16 && ctx->impl == FSHARP_IMPL_AUTO ? TC : FMA;
+  else if (ctx->impl == FSHARP_IMPL_SIMT) p.kind = FMA;
+  else p.kind = bf16 ? TC : parts_fit(dm) && R > FMA_MOST_ROWS ? TC32 : FMA;
   if (dm->Lk == 0) p.kind = FMA;       // (zeros: there is no key that a tensor map could describe)
   bool cluster = false;
-  p.pieces = p.kind == ROWS ? fs_cross_rows_pieces(ctx, dm, dtype, &cluster) : p.kind == TC ? fs_tc_cross_pieces(ctx, dm) : fs_cross_fma_pieces(ctx, dm);
+  switch (p.kind) {
+    case ROWS: p.pieces = fs_cross_rows_pieces(ctx, dm, dtype, &cluster); break;
+    case FMA: p.pieces = fs_cross_fma_pieces(ctx, dm); break;
+    case TC: p.pieces = fs_tc_cross_pieces(ctx, dm); break;
+    case TC32: p.pieces = fs_tc_cross_f32_pieces(ctx, dm); p.parts = fs_tc_cross_f32_parts(dm, 0); break;
+  }
   p.join = p.pieces > 1 && !cluster;
   if (p.join) {
     p.ml = units * p.pieces * R;
@@ -135,15 +148,20 @@ Plan plan_forward(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype)
 }
 
 struct GradPlan {
-  bool tc;
+  Kind kind;
+  int64_t parts;
   int kv_pieces, q_pieces;
   int64_t stat, kv_floats, q_floats;
 };
 GradPlan plan_backward(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype) {
   GradPlan p = {};
   const int64_t R = (int64_t)dm->H / dm->Hk * dm->Lq, units = (int64_t)dm->B * dm->Hk;
-  p.tc = dtype == FSHARP_BF16 && ctx->impl != FSHARP_IMPL_SIMT && dm->Lk > 0;
-  (p.tc ? fs_tc_cross_grad_pieces : fs_cross_fma_grad_pieces)(ctx, dm, &p.kv_pieces, &p.q_pieces);
+  p.kind = FMA;
+  if (ctx->impl != FSHARP_IMPL_SIMT && dm->Lk > 0) p.kind = dtype == FSHARP_BF16 ? TC : parts_fit(dm) ? TC32 : FMA;
+  if (p.kind == TC) fs_tc_cross_grad_pieces(ctx, dm, &p.kv_pieces, &p.q_pieces);
+  else if (p.kind == TC32) fs_tc_cross_f32_grad_pieces(ctx, dm, &p.kv_pieces, &p.q_pieces);
+  else fs_cross_fma_grad_pieces(ctx, dm, &p.kv_pieces, &p.q_pieces);
+  if (p.kind == TC32) p.parts = fs_tc_cross_f32_parts(dm, 1);
   p.stat = (int64_t)dm->B * dm->H * cross_stat_floats(dm->Lq);
   if (p.kv_pieces > 1) p.kv_floats = p.kv_pieces * units * dm->Lk * (dm->d + dm->dv);
   if (p.q_pieces > 1) p.q_floats = p.q_pieces * units * R * dm->d;
@@ -163,8 +181,8 @@ CrossArgs args_of(const fsharp_cross_dims* dm, const void* Q, const void* K, con
   return a;
 }
 
-int64_t forward_bytes(const Plan& p) { return p.join ? (int64_t)(ws_round(p.o_floats * 4) + ws_round(p.ml * 8)) : 0; }
-int64_t backward_bytes(const GradPlan& p) { return (int64_t)(ws_round(p.stat * 4) + ws_round(p.kv_floats * 4) + ws_round(p.q_floats * 4)); }
+int64_t forward_bytes(const Plan& p) { return (int64_t)((p.join ? ws_round(p.o_floats * 4) + ws_round(p.ml * 8) : 0) + ws_round(p.parts * 2)); }
+int64_t backward_bytes(const GradPlan& p) { return (int64_t)(ws_round(p.stat * 4) + ws_round(p.kv_floats * 4) + ws_round(p.q_floats * 4) + ws_round(p.parts * 2)); }
 
 int check_scratch(const void* scratch, int64_t have, int64_t need) {
   if (need == 0) return FSHARP_OK;
@@ -204,13 +222,14 @@ int fsharp_cross_attend(fsharp_ctx* ctx, const void* Q, const void* K, const voi
   const CrossArgs a = args_of(dims, Q, K, V, key_len, key_mask, scale);
   const TensorAddr ay = fs_addr(dims->y_stride, dims->H, dims->Lq, dims->dv);
   CrossPart part = {nullptr, nullptr, p.pieces};
+  WsAlloc ws{static_cast<char*>(scratch), 0};
   if (p.join) {
-    WsAlloc ws{static_cast<char*>(scratch), 0};
     part.o = ws.take<float>(p.o_floats);
     part.ml = ws.take<float2>(p.ml);
   }
   if (p.kind == ROWS) FS_TRY(fs_cross_rows(ctx, a, dtype, Y, ay, lse, part));
   else if (p.kind == TC) FS_TRY(fs_tc_cross(ctx, a, Y, ay, lse, part));
+  else if (p.kind == TC32) FS_TRY(fs_tc_cross_f32(ctx, a, Y, ay, lse, part, ws.take<char>(p.parts * 2)));
   else FS_TRY(fs_cross_fma(ctx, a, dtype, Y, ay, lse, part));
   return p.join ? fs_cross_join(ctx, a, dtype, Y, ay, lse, part) : FSHARP_OK;
 }
@@ -257,7 +276,9 @@ int fsharp_cross_attend_backward(fsharp_ctx* ctx, const void* Q, const void* K, 
   const TensorAddr ay = fs_addr(dims->y_stride, dims->H, dims->Lq, dims->dv);
   const bool f32 = dtype == FSHARP_F32;
   FS_TRY(f32 ? run_delta<float>(ctx, a, Y, ay, dY, gr.ady, lse, stat) : run_delta<__nv_bfloat16>(ctx, a, Y, ay, dY, gr.ady, lse, stat));
-  FS_TRY(p.tc ? fs_tc_cross_grad(ctx, a, gr) : fs_cross_fma_grad(ctx, a, dtype, gr));
+  if (p.kind == TC) FS_TRY(fs_tc_cross_grad(ctx, a, gr));
+  else if (p.kind == TC32) FS_TRY(fs_tc_cross_f32_grad(ctx, a, gr, ws.take<char>(p.parts * 2)));
+  else FS_TRY(fs_cross_fma_grad(ctx, a, dtype, gr));
   const auto sum = f32 ? run_sum<float> : run_sum<__nv_bfloat16>;
   const int64_t keys = (int64_t)a.B * a.Hk * a.Lk;
   if (gr.pkv) {

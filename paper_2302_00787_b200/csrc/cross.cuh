@@ -46,6 +46,11 @@ int fs_cross_join(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, Tenso
 int fs_cross_fma_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm);
 int fs_cross_fma(fsharp_ctx* ctx, const CrossArgs& a, int dtype, void* Y, TensorAddr ay, float* lse, CrossPart part);
 
+// fp32, d and dv up to 64, on the tensor cores (tc_cross_f32.cu); scratch: the parts of the operands
+int fs_tc_cross_f32_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm);
+int64_t fs_tc_cross_f32_parts(const fsharp_cross_dims* dm, int backward);
+int fs_tc_cross_f32(fsharp_ctx* ctx, const CrossArgs& a, void* Y, TensorAddr ay, float* lse, CrossPart part, void* scratch);
+
 // Backward.  stat [B][H][ceil(Lq / 128)][2][128]: 128 rows' -lse log2(e), then their -D; rows that see nothing and places behind the last
 // row have -inf and 0, which makes every 2^(x - lse) of theirs zero.  Partial sums of a piece: dK | dV [piece][unit][Lk][d + dv], dQ [piece][unit][R][d].
 struct CrossGrad {
@@ -66,5 +71,7 @@ __device__ __forceinline__ float2 cross_stat(const float* stat, int64_t bh, int 
 // tensor cores (tc_cross_bwd.cu): bf16
 void fs_tc_cross_grad_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int* kv_pieces, int* q_pieces);
 int fs_tc_cross_grad(fsharp_ctx* ctx, const CrossArgs& a, const CrossGrad& gr);
+void fs_tc_cross_f32_grad_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int* kv_pieces, int* q_pieces);
+int fs_tc_cross_f32_grad(fsharp_ctx* ctx, const CrossArgs& a, const CrossGrad& gr, void* scratch);
 void fs_cross_fma_grad_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int* kv_pieces, int* q_pieces);
 int fs_cross_fma_grad(fsharp_ctx* ctx, const CrossArgs& a, int dtype, const CrossGrad& gr);

@@ -184,6 +184,7 @@ const char* fsharp_kernel_name(int id) {
     case FS_K_CROSS_DKV: return "cross_dkv_kernel";
     case FS_K_CROSS_DQ: return "cross_dq_kernel";
     case FS_K_CROSS_SUM: return "cross_sum_kernel";
+    case FS_K_CROSS_SPLIT: return "cross_split_kernel";
     case FS_K_TC_CROSS: return "tc_cross_kernel";
     case FS_K_TC_CROSS_DKV: return "tc_cross_dkv_kernel";
     case FS_K_TC_CROSS_DQ: return "tc_cross_dq_kernel";

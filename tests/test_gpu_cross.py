@@ -97,8 +97,6 @@ def check_lse(lse, ref, d):
 @pytest.mark.parametrize("impl", (fb.IMPL_AUTO, fb.IMPL_SIMT), ids=("auto", "simt"))
 @pytest.mark.parametrize("case", CASES, ids=NAMES)
 def test_forward(ctx, case, dtype, impl):
-    if dtype == F32 and impl == fb.IMPL_SIMT:
-        pytest.skip("fp32 has one kernel family")
     Q, K, V, _, kw, ref = make(case, dtype)
     ctx.set_impl(impl)
     try:
@@ -118,8 +116,6 @@ def test_forward(ctx, case, dtype, impl):
 @pytest.mark.parametrize("impl", (fb.IMPL_AUTO, fb.IMPL_SIMT), ids=("auto", "simt"))
 @pytest.mark.parametrize("case", CASES, ids=NAMES)
 def test_backward(ctx, case, dtype, impl):
-    if dtype == F32 and impl == fb.IMPL_SIMT:
-        pytest.skip("fp32 has one kernel family")
     Q, K, V, dY, kw, ref = make(case, dtype, 1)
     ctx.set_impl(impl)
     try:
