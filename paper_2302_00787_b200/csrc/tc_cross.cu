@@ -7,10 +7,13 @@
 // products: S of the next tile and P V of one warpgroup run while the other one is at its exponentials.
 // With more than 128 rows the warpgroups take 128 rows each and share every K and V tile; with fewer they take the tiles in
 // turn, as if one were another piece of the keys, and meet in shared memory at the end.
-// O is only rescaled when a row's maximum has grown by more than 2^8 (every factor is exact in the sense that l and O have the
-// same one); P is then at most 2^8, which bf16 holds as well as 1.
+// O is only rescaled when a row's maximum has grown by more than 2^8 (l and O always have the same factor); P is then at most 2^8,
+// which bf16 holds as well as 1.
 // P is rounded to bf16 (2^-8 relative) as the tensor core's operand; l sums the exponentials before that rounding, in fp32.
-// Bound: exponentials (128 x 128 per tile and warpgroup; part of them by a cubic on the multiply-add pipe) and issue slots.
+// Bound: exponentials (128 x 128 per tile and warpgroup at 16 per clock, one in eight by a cubic on the multiply-add pipe) and the
+// instructions around them.  4 x 12 x 4096 queries, 8192 keys, d = 64: 626 us, 658 TFLOP/s, at 1965 MHz and 940 W of 1000; without the
+// warpgroups' arithmetic 441 us.  (Two threads per row, half of the keys each, 16 warps: 679 us; two blocks per SM with tiles of 64
+// keys: 726 us.)
 #include "cross.cuh"
 #include "tc_common.cuh"
 #include "tc_cross.cuh"
@@ -26,9 +29,6 @@ constexpr int CX_WARPS = 8, CXW_TMA = 8, CXW_MMA = 9, CX_T = 384;      // (warps
 constexpr int CX_REGS_REST = 56, CX_REGS_ROWS = 224;                   // 384 threads x 168 at launch = 128 x 56 + 256 x 224
 constexpr uint32_t CX_TMEM = 512;
 constexpr float CX_SLACK = 8.f;
-#ifndef CX_CUBIC
-#define CX_CUBIC 1
-#endif
 
 template <int D>
 struct CxSm {
@@ -280,7 +280,7 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
 #pragma unroll
           for (int k = 0; k < 32; k += 2) {
             fma2(s[q + k], s[q + k + 1], c, base);
-            if ((k & 15) < 16 - 2 * CX_CUBIC) {
+            if ((k & 15) < 14) {                             // (one pair of eight by the cubic: 626 us; none 647, two 632, three 686)
               s[q + k] = __float_as_uint(ex2(__uint_as_float(s[q + k])));
               s[q + k + 1] = __float_as_uint(ex2(__uint_as_float(s[q + k + 1])));
             } else {
@@ -352,17 +352,7 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
           if (!both) x[k] = x[k] * f0 + xo[row * (D + 1) + q + k] * f1;
           x[k] *= inv;
         }
-        if (r < R) {
-          if (part.pieces > 1) {
-#pragma unroll
-            for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(part.o + at * a.dv + q + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
-          } else {
-#pragma unroll
-            for (int k = 0; k < 16; k += 8)
-              *reinterpret_cast<uint4*>(y + q + k) = make_uint4(pack_bf16(x[k], x[k + 1]), pack_bf16(x[k + 2], x[k + 3]), pack_bf16(x[k + 4], x[k + 5]), pack_bf16(x[k + 6], x[k + 7]));
-          }
-        }
-        __syncwarp();
+        store_row(r < R, x, part.pieces > 1 ? part.o + at * a.dv + q : nullptr, y + q);
       }
       if (r < R) {
         if (part.pieces > 1) part.ml[at] = make_float2(m, sum);

@@ -55,4 +55,24 @@ __device__ __forceinline__ void issue_cols(uint32_t d_tmem, uint32_t a_tmem, Des
   for (int k = 0; k < STEPS; k++) tc::mma_bf16_ta_lh(d_tmem, a_tmem + 8 * k, b.lo + k * (2048 / 16), b.hi, idesc, k > 0 ? 1u : accumulate);
 }
 
+// The same with A [128 x T] in two halves of T / 2 whose columns begin APART columns from each other
+template <int T, int APART>
+__device__ __forceinline__ void issue_halves(uint32_t d_tmem, uint32_t a_tmem, Desc b, uint32_t idesc, uint32_t accumulate) {
+#pragma unroll
+  for (int k = 0; k < T / 16; k++)
+    tc::mma_bf16_ta_lh(d_tmem, a_tmem + k / (T / 32) * APART + k % (T / 32) * 8, b.lo + k * (2048 / 16), b.hi, idesc, k > 0 ? 1u : accumulate);
+}
+
+// 16 values of a row, all of its warp's lanes together: to fp32 sums of a piece, or rounded to the gradient.
+__device__ __forceinline__ void store_row(bool on, const float (&x)[16], float* part, __nv_bfloat16* out) {
+  if (on && part) {
+#pragma unroll
+    for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(part + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+  } else if (on) {
+#pragma unroll
+    for (int k = 0; k < 16; k += 8)
+      *reinterpret_cast<uint4*>(out + k) = make_uint4(tc::pack_bf16(x[k], x[k + 1]), tc::pack_bf16(x[k + 2], x[k + 3]), tc::pack_bf16(x[k + 4], x[k + 5]), tc::pack_bf16(x[k + 6], x[k + 7]));
+  }
+  __syncwarp();
+}
 }  // namespace tcx

@@ -33,19 +33,6 @@ __device__ __forceinline__ void exps2(uint32_t& x, uint32_t& y, bool cubic) {
   else { x = __float_as_uint(ex2(__uint_as_float(x))); y = __float_as_uint(ex2(__uint_as_float(y))); }
 }
 
-// 16 values of a row, all of its warp's lanes together: to fp32 sums of a piece, or rounded to the gradient.
-__device__ __forceinline__ void store_row(bool on, const float (&x)[16], float* part, __nv_bfloat16* out) {
-  if (on && part) {
-#pragma unroll
-    for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(part + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
-  } else if (on) {
-#pragma unroll
-    for (int k = 0; k < 16; k += 8)
-      *reinterpret_cast<uint4*>(out + k) = make_uint4(pack_bf16(x[k], x[k + 1]), pack_bf16(x[k + 2], x[k + 3]), pack_bf16(x[k + 4], x[k + 5]), pack_bf16(x[k + 6], x[k + 7]));
-  }
-  __syncwarp();
-}
-
 // ------------------------------------------------------------------------------------------ dK, dV
 // The products of a tile are issued so that what the warpgroups make is wanted two products later: dV, next S^T, dK, next dP^T; each
 // warpgroup has half of a tile's rows.  At d = 64 two blocks on an SM, tiles of 64 rows, hide each other's starts and ends (16 x 12 x 512 x
@@ -67,14 +54,6 @@ struct KvMs {
   int abort_flag;
 };
 static_assert(sizeof(KvMs) <= 512, "misc block");
-
-// A = P^T or dS^T [128 x T] in tensor memory (its two halves T / 2 columns apart) times the tile's T rows in shared memory
-template <int T>
-__device__ __forceinline__ void issue_halves(uint32_t d_tmem, uint32_t a_tmem, Desc b, uint32_t idesc, uint32_t accumulate) {
-#pragma unroll
-  for (int k = 0; k < T / 16; k++)
-    mma_bf16_ta_lh(d_tmem, a_tmem + k / (T / 32) * (T / 2) + k % (T / 32) * 8, b.lo + k * (2048 / 16), b.hi, idesc, k > 0 ? 1u : accumulate);
-}
 
 template <int D>
 __global__ void __launch_bounds__(CG_T, KvSm<D>::BLOCKS)
@@ -196,7 +175,7 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       if (leader) {
         Desc g = gt;
         g.lo += s * (Sm::TILE_D / 16);
-        issue_halves<T>(tmem + Sm::DV, tmem + Sm::S, g, ID_V, i > 0);
+        issue_halves<T, T / 2>(tmem + Sm::DV, tmem + Sm::S, g, ID_V, i > 0);
         mma_commit(&misc->g_empty[s]);
       }
       __syncwarp();
@@ -206,7 +185,7 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       if (leader) {
         Desc q = qt;
         q.lo += s * (Sm::TILE_D / 16);
-        issue_halves<T>(tmem + Sm::DK, tmem + Sm::P, q, ID_K, i > 0);
+        issue_halves<T, T / 2>(tmem + Sm::DK, tmem + Sm::P, q, ID_K, i > 0);
         mma_commit(&misc->q_empty[s]);
         if (i == items - 1) mma_commit(&misc->done);
       }

@@ -31,23 +31,37 @@ constexpr uint32_t CF_TMEM = 512;
 __device__ constexpr int PA[6] = {2, 0, 1, 1, 0, 0}, PB[6] = {0, 2, 1, 0, 1, 0};
 
 // ------------------------------------------------------------------------------------------ parts
-// x [B,H,L,d] fp32 -> its parts [3][B H][L][d] bf16, eight values per thread
+// Up to four tensors x [B,H,L,d] fp32 -> their parts [3][B H][L][d] bf16, one after the other; eight values per thread.
+struct SplitJob {
+  const float* x;
+  TensorAddr ax;
+  int64_t rows, end;           // rows of all heads; threads of this tensor and of those before it
+  __nv_bfloat16* parts;
+  int H, L, d;
+};
+struct SplitJobs {
+  SplitJob job[4];
+};
 __global__ void __launch_bounds__(256)
-cross_split_kernel(const float* __restrict__ x, TensorAddr ax, int64_t rows, int H, int L, int d, __nv_bfloat16* __restrict__ parts) {
-  const int q = d / 8;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / q;
-  if (row >= rows) return;
-  const int e = (int)(i % q) * 8;
-  const float* p = x + row / ((int64_t)H * L) * ax.sb + row / L % H * ax.sh + row % L * ax.sl + e;
+cross_split_kernel(const __grid_constant__ SplitJobs jobs, int n) {
+  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  int t = 0;
+  while (t < n && i >= jobs.job[t].end) t++;
+  if (t == n) return;
+  const SplitJob& j = jobs.job[t];
+  if (t) i -= jobs.job[t - 1].end;
+  const int q = j.d / 8, e = (int)(i % q) * 8;
+  const int64_t row = i / q;
+  const float* p = j.x + row / ((int64_t)j.H * j.L) * j.ax.sb + row / j.L % j.H * j.ax.sh + row % j.L * j.ax.sl + e;
   float v[8];
   *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
   *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(p + 4);
   uint4 h, m, l;
   split3::split8(v, h, m, l);
-  const int64_t n = rows * d, at = row * d + e;
-  *reinterpret_cast<uint4*>(parts + at) = h;
-  *reinterpret_cast<uint4*>(parts + n + at) = m;
-  *reinterpret_cast<uint4*>(parts + 2 * n + at) = l;
+  const int64_t all = j.rows * j.d, at = row * j.d + e;
+  *reinterpret_cast<uint4*>(j.parts + at) = h;
+  *reinterpret_cast<uint4*>(j.parts + all + at) = m;
+  *reinterpret_cast<uint4*>(j.parts + 2 * all + at) = l;
 }
 
 // Rows r0 .. r0 + 127 of a unit's packed rows of X, split, into a [3][128 x 64] tile by 256 threads (thread `t`).
@@ -812,20 +826,35 @@ tc_cross_f32_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
   }
 }
 
-int split(fsharp_ctx* ctx, const void* x, TensorAddr ax, int B, int H, int L, int d, __nv_bfloat16* parts) {
-  const int64_t rows = (int64_t)B * H * L, blocks = (rows * (d / 8) + 255) / 256;
-  if (blocks > 0x7fffffff) return FSHARP_E_SHAPE;
-  FS_TIME_BEGIN(ctx, FS_K_CROSS_SPLIT);
-  cross_split_kernel<<<(unsigned)blocks, 256, 0, ctx->stream>>>(static_cast<const float*>(x), ax, rows, H, L, d, parts);
-  FS_TIME_END(ctx);
-  FS_LAUNCH_CHECK(ctx);
-  return FSHARP_OK;
-}
+int64_t parts_of(int64_t rows, int d) { return 3 * rows * d; }
+// Collects tensors to split; `next` is where the next one's parts go.
+struct Split {
+  SplitJobs jobs;
+  int n = 0;
+  int64_t threads = 0;
+  __nv_bfloat16* next;
+  __nv_bfloat16* add(const void* x, TensorAddr ax, int B, int H, int L, int d) {
+    __nv_bfloat16* parts = next;
+    const int64_t rows = (int64_t)B * H * L;
+    threads += rows * (d / 8);
+    next += parts_of(rows, d);
+    jobs.job[n++] = SplitJob{static_cast<const float*>(x), ax, rows, threads, parts, H, L, d};
+    return parts;
+  }
+  int run(fsharp_ctx* ctx) {
+    const int64_t blocks = (threads + 255) / 256;
+    if (blocks > 0x7fffffff) return FSHARP_E_SHAPE;
+    FS_TIME_BEGIN(ctx, FS_K_CROSS_SPLIT);
+    cross_split_kernel<<<(unsigned)blocks, 256, 0, ctx->stream>>>(jobs, n);
+    FS_TIME_END(ctx);
+    FS_LAUNCH_CHECK(ctx);
+    return FSHARP_OK;
+  }
+};
 // parts [3][B H][L][d]
 int parts_map(CUtensorMap* map, const __nv_bfloat16* parts, int BH, int L, int d, int rows) {
   return fs_tc_cross_map(map, parts, TensorAddr{(int64_t)BH * L * d, (int64_t)L * d, d}, 3, BH, L, d, rows);
 }
-int64_t parts_of(int64_t rows, int d) { return 3 * rows * d; }
 int pieces_for(const fsharp_ctx* ctx, int64_t blocks, int64_t most) {
   int64_t p = ctx->sm_count / blocks;
   if (p > most) p = most;
@@ -845,9 +874,10 @@ int64_t fs_tc_cross_f32_parts(const fsharp_cross_dims* dm, int backward) {
   return parts_of(keys, dm->d) + parts_of(keys, dm->dv) + (backward ? parts_of(rows, dm->d) + parts_of(rows, dm->dv) : 0);
 }
 int fs_tc_cross_f32(fsharp_ctx* ctx, const CrossArgs& a, void* Y, TensorAddr ay, float* lse, CrossPart part, void* scratch) {
-  __nv_bfloat16 *pk = static_cast<__nv_bfloat16*>(scratch), *pv = pk + parts_of((int64_t)a.B * a.Hk * a.Lk, a.d);
-  FS_TRY(split(ctx, a.K, a.ak, a.B, a.Hk, a.Lk, a.d, pk));
-  FS_TRY(split(ctx, a.V, a.av, a.B, a.Hk, a.Lk, a.dv, pv));
+  Split split;
+  split.next = static_cast<__nv_bfloat16*>(scratch);
+  const __nv_bfloat16 *pk = split.add(a.K, a.ak, a.B, a.Hk, a.Lk, a.d), *pv = split.add(a.V, a.av, a.B, a.Hk, a.Lk, a.dv);
+  FS_TRY(split.run(ctx));
   CUtensorMap tmK, tmV;
   FS_TRY(parts_map(&tmK, pk, a.B * a.Hk, a.Lk, a.d, KT));
   FS_TRY(parts_map(&tmV, pv, a.B * a.Hk, a.Lk, a.dv, KT));
@@ -866,12 +896,11 @@ void fs_tc_cross_f32_grad_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims*
   *q_pieces = pieces_for(ctx, units * ((g * dm->Lq + TILE - 1) / TILE), kt);
 }
 int fs_tc_cross_f32_grad(fsharp_ctx* ctx, const CrossArgs& a, const CrossGrad& gr, void* scratch) {
-  const int64_t keys = (int64_t)a.B * a.Hk * a.Lk, rows = (int64_t)a.B * a.H * a.Lq;
-  __nv_bfloat16 *pk = static_cast<__nv_bfloat16*>(scratch), *pv = pk + parts_of(keys, a.d), *pq = pv + parts_of(keys, a.dv), *pg = pq + parts_of(rows, a.d);
-  FS_TRY(split(ctx, a.K, a.ak, a.B, a.Hk, a.Lk, a.d, pk));
-  FS_TRY(split(ctx, a.V, a.av, a.B, a.Hk, a.Lk, a.dv, pv));
-  FS_TRY(split(ctx, a.Q, a.aq, a.B, a.H, a.Lq, a.d, pq));
-  FS_TRY(split(ctx, gr.dY, gr.ady, a.B, a.H, a.Lq, a.dv, pg));
+  Split split;
+  split.next = static_cast<__nv_bfloat16*>(scratch);
+  const __nv_bfloat16 *pk = split.add(a.K, a.ak, a.B, a.Hk, a.Lk, a.d), *pv = split.add(a.V, a.av, a.B, a.Hk, a.Lk, a.dv),
+                      *pq = split.add(a.Q, a.aq, a.B, a.H, a.Lq, a.d), *pg = split.add(gr.dY, gr.ady, a.B, a.H, a.Lq, a.dv);
+  FS_TRY(split.run(ctx));
   CUtensorMap tmQ, tmG, tmK, tmV, tmKt, tmVt;
   FS_TRY(parts_map(&tmQ, pq, a.B * a.H, a.Lq, a.d, KT));
   FS_TRY(parts_map(&tmG, pg, a.B * a.H, a.Lq, a.dv, KT));
