@@ -1,6 +1,6 @@
 // Cross attention of few query rows per key head (decoding steps): K and V are streamed once.  A key's d values lie across
-// D / VE lanes (16 bytes each), a warp's copy covers 512 bytes of K or V, and asynchronous copies of up to three turns of four keys
-// and values per lane are in flight (up to 190 KB per SM); scores are sums over a key's lanes by shuffles.
+// D / VE lanes (16 bytes each), a warp's copy covers 512 bytes of K or V, and asynchronous copies of a few turns of keys and values per lane
+// are in flight (up to 190 KB per SM); scores are sums over a key's lanes by shuffles.
 // Each lane group keeps a maximum, a sum and an output of its own; they meet once at the end: warp, block, then the pieces of
 // the keys, which are the blocks of a cluster (up to eight; one launch) or meet in scratch (cross_join_kernel).
 // Bound: HBM (2 n d values per unit).
@@ -9,8 +9,11 @@
 
 namespace {
 
-constexpr int RW_T = 128, RW_WARPS = RW_T / 32, RW_U = 4, RW_STAGES = 3;
-constexpr size_t RW_RING = (size_t)RW_STAGES * 2 * RW_U * RW_T * 16;      // 48 KB: four blocks on an SM
+constexpr int RW_T = 128, RW_WARPS = RW_T / 32;
+// Keys per lane and turn, and turns in flight: 32 KB of copies per block, six blocks on an SM; heads of 128, whose turns are half as many
+// keys, 48 KB.  (64 x 12 sequences of 1500 keys, d = 64: 53 us so, 62 with 4 and 3; 16 x 8 of 16384, d = 128: 176 with 4 and 3, 208 with 2 and 4.)
+__host__ __device__ constexpr int rows_u(int D) { return D == 128 ? 4 : 2; }
+__host__ __device__ constexpr int rows_stages(int D) { return D == 128 ? 3 : 4; }
 constexpr int RW_CLUSTER = 8;      // most pieces that meet in a cluster
 
 template <typename T> __device__ __forceinline__ void widen(const uint4& x, float* v);
@@ -23,12 +26,12 @@ template <> __device__ __forceinline__ void widen<__nv_bfloat16>(const uint4& x,
   for (int i = 0; i < 4; i++) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
 }
 
-__host__ __device__ constexpr int rows_step(int D, int es) { return RW_WARPS * (32 / (D * es / 16)) * RW_U; }    // keys per turn of a block
+__host__ __device__ constexpr int rows_step(int D, int es) { return RW_WARPS * (32 / (D * es / 16)) * rows_u(D); }    // keys per turn of a block
 
 template <typename T, int D, int R>
 __global__ void __launch_bounds__(RW_T)
 cross_rows_kernel(const __grid_constant__ CrossArgs a, T* __restrict__ Y, TensorAddr ay, float* __restrict__ lse, CrossPart part) {
-  constexpr int VE = 16 / (int)sizeof(T), LPK = D / VE, KPW = 32 / LPK, STEP = RW_WARPS * KPW * RW_U;
+  constexpr int RW_U = rows_u(D), RW_STAGES = rows_stages(D), VE = 16 / (int)sizeof(T), LPK = D / VE, KPW = 32 / LPK, STEP = RW_WARPS * KPW * RW_U;
   static_assert(STEP == rows_step(D, sizeof(T)), "");
   __shared__ float so[RW_WARPS][R][D];
   __shared__ float sm[RW_WARPS][R], sl[RW_WARPS][R];
@@ -256,7 +259,7 @@ int launch_rows(fsharp_ctx* ctx, const CrossArgs& a, T* Y, TensorAddr ay, float*
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)part.pieces, (unsigned)(a.B * a.Hk));
   cfg.blockDim = dim3(RW_T);
-  cfg.dynamicSmemBytes = RW_RING;
+  cfg.dynamicSmemBytes = (size_t)rows_stages(D) * 2 * rows_u(D) * RW_T * 16;
   cfg.stream = ctx->stream;
   cudaLaunchAttribute at[1];
   if (!part.o && part.pieces > 1) {
@@ -303,16 +306,16 @@ int run_join(fsharp_ctx* ctx, const CrossArgs& a, T* Y, TensorAddr ay, float* ls
 // price of one: 16 x 4 key heads, 16384 keys, d = 128: 182 us here and 165 there for one row, 249 and 90 for two), four of fp32.
 int fs_cross_rows_most(int dtype) { return dtype == FSHARP_F32 ? 4 : 1; }
 
-// Pieces of the keys: enough for twelve blocks per SM, which even out sequences of different lengths, each with two turns of keys
-// where eight pieces (a cluster) do; where they leave SMs without work, as many more, through scratch, as give every SM four blocks.
+// Pieces of the keys: enough for six blocks per SM, each with two turns of keys, where eight pieces (a cluster, which joins them
+// itself) do; where they leave SMs without work, as many more, through scratch, as give every SM two blocks.
 int fs_cross_rows_pieces(const fsharp_ctx* ctx, const fsharp_cross_dims* dm, int dtype, bool* cluster) {
   const int es = dtype == FSHARP_F32 ? 4 : 2, D = dm->d > dm->dv ? dm->d : dm->dv, step = rows_step(D, es);
   const int64_t units = (int64_t)dm->B * dm->Hk, turns = ((int64_t)dm->Lk + step - 1) / step, sms = ctx->sm_count;
-  int64_t p = (12 * sms + units - 1) / units;
+  int64_t p = (6 * sms + units - 1) / units;
   if (p > turns / 2) p = turns / 2;
   *cluster = p <= RW_CLUSTER || units * RW_CLUSTER >= 2 * sms;
   if (*cluster) p = p > RW_CLUSTER ? RW_CLUSTER : p;
-  else p = p < 4 * sms / units ? p : 4 * sms / units;
+  else p = p < 2 * sms / units ? p : 2 * sms / units;
   return p < 1 ? 1 : p > 256 ? 256 : (int)p;
 }
 
