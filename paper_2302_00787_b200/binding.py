@@ -159,26 +159,28 @@ def _strides(t: torch.Tensor):
 
 
 _INNER_ONLY = {torch.float32: 3, torch.bfloat16: 7}      # element strides are multiples of 16 bytes: these bits are zero
+_NO_STRIDES = (0, 0, 0)
 _CROSS_DIMS = struct.Struct("=7i4x25q")                  # fsharp_cross_dims, packed
 _ROTATE_DIMS = struct.Struct("=5i4x12q")                 # fsharp_rotate_dims, packed
 
 
 def _place(t: torch.Tensor):
-    """(t, its strides of batch, head and token), or those of a dense copy where the library cannot be told t's: a tensor
-    broadcast along every dimension (three zeros mean dense there) or along its tokens, rows or a start that are not
-    16-byte aligned, a last dimension with gaps.  Dimensions of size one get a dense tensor's stride: nothing reads it."""
+    """(t, its strides of batch, head and token, its address), or those of a dense copy where the library cannot be told
+    t's: a tensor broadcast along every dimension (three zeros mean dense there) or along its tokens, rows or a start that
+    are not 16-byte aligned, a last dimension with gaps.  Dimensions of size one get a dense tensor's stride: nothing
+    reads it."""
     b, h, l, e = t.stride()
-    low = _INNER_ONLY[t.dtype]
-    if e == 1 and b and h and l and not (b | h | l) & low and not t.data_ptr() & 15:
-        return t, (b, h, l)
+    low, at = _INNER_ONLY[t.dtype], t.data_ptr()
+    if e == 1 and b and h and l and not (b | h | l) & low and not at & 15:
+        return t, (b, h, l), at
     B, H, L, inner = t.shape
     if B * H * L * inner == 0:
-        return t, (H * L * inner, L * inner, inner)
+        return t, (H * L * inner, L * inner, inner), at
     own = (b if B > 1 else H * L * inner, h if H > 1 else L * inner, l if L > 1 else inner)
-    if (e != 1 and inner > 1) or own[2] == 0 or not any(own) or (own[0] | own[1] | own[2]) & low or t.data_ptr() & 15:
+    if (e != 1 and inner > 1) or own[2] == 0 or not any(own) or (own[0] | own[1] | own[2]) & low or at & 15:
         t = t.clone(memory_format=torch.contiguous_format)
-        return t, t.stride()[:3]
-    return t, own
+        return t, t.stride()[:3], t.data_ptr()
+    return t, own, at
 
 
 def _check_written(name: str, t: torch.Tensor) -> None:
@@ -404,19 +406,23 @@ class Context:
         """Rotary positions (make_rope) on Q [B,H,L,d] and K [B,Hk,L,d] (K may be None): (Q', K').  pos: int64 [B,L] or
         [L], None for 0 .. L-1; pos0 is added to it.  transpose: the gradient.  out: a pair of tensors to write, Q and K
         themselves among them; the default is new dense ones."""
-        self._mine(Q=Q, K=K, pos=pos)
+        here = self.device
+        if Q.get_device() != here or (K is not None and K.get_device() != here) or (pos is not None and pos.get_device() != here):
+            self._mine(Q=Q, K=K, pos=pos)
         dt = _dtype_code(Q)
-        B, H, L, d = Q.shape
-        if K is not None and (K.dim() != 4 or K.shape[0] != B or K.shape[2:] != Q.shape[2:] or K.dtype != Q.dtype):
-            raise ValueError(f"K: expected {(B, 'Hk', L, d)} of {Q.dtype}, got {tuple(K.shape)} of {K.dtype}")
-        pos_stride = 0
+        B, H, L, d = shape = Q.shape
+        Hk, pos_at, pos_stride = 0, None, 0
+        if K is not None:
+            Bk, Hk, Lk, dk = K.shape
+            if Bk != B or Lk != L or dk != d or K.dtype != Q.dtype:
+                raise ValueError(f"K: expected {(B, 'Hk', L, d)} of {Q.dtype}, got {tuple(K.shape)} of {K.dtype}")
         if pos is not None:
             if pos.dtype != torch.int64 or tuple(pos.shape) not in ((B, L), (L,)) or (L > 1 and pos.stride(-1) != 1):
                 raise ValueError("pos: expected int64 [B, L] or [L] whose last dimension is contiguous")
-            pos_stride = pos.stride(0) if pos.dim() == 2 else 0
+            pos_at, pos_stride = pos.data_ptr(), pos.stride(0) if pos.dim() == 2 else 0
         if out is None:
-            Qo = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
-            Ko = None if K is None else torch.empty(K.shape, dtype=K.dtype, device=K.device)
+            Qo, so = Q.new_empty(shape), (H * L * d, L * d, d)
+            Ko, sz = (None, _NO_STRIDES) if K is None else (K.new_empty(K.shape), (Hk * L * d, L * d, d))
         else:
             Qo, Ko = out
             self._mine(out=Qo, out_k=Ko)
@@ -425,38 +431,45 @@ class Context:
                     if y is None or y.shape != x.shape or y.dtype != x.dtype:
                         raise ValueError("out: expected the shapes and type of Q and K")
                     _check_written("out", y)
-        Q, sq = _place(Q)
-        so = _written_place(Qo)
-        qp, kp, yp, zp = Q.data_ptr(), None, Qo.data_ptr(), None
-        Hk, sk, sz = 0, (0, 0, 0), (0, 0, 0)
+            so, sz = _written_place(Qo), _NO_STRIDES if K is None else _written_place(Ko)
+        Q, sq, q_at = _place(Q)
+        sk, k_at, ko_at = _NO_STRIDES, None, None
         if K is not None:
-            K, sk = _place(K)
-            sz = _written_place(Ko)
-            Hk, kp, zp = K.shape[1], K.data_ptr(), Ko.data_ptr()
-        rc = self.lib.fsharp_rotate(self._h, qp, kp, None if pos is None else pos.data_ptr(), pos_stride, pos0, rope,
-                                    _ROTATE_DIMS.pack(B, L, H, Hk, d, *sq, *sk, *so, *sz), dt, 1 if transpose else 0, yp, zp)
+            K, sk, k_at = _place(K)
+            ko_at = Ko.data_ptr()
+        rc = self.lib.fsharp_rotate(self._h, q_at, k_at, pos_at, pos_stride, pos0, rope,
+                                    _ROTATE_DIMS.pack(B, L, H, Hk, d, *sq, *sk, *so, *sz), dt, 1 if transpose else 0,
+                                    Qo.data_ptr(), ko_at)
         if rc:
             raise FsharpError(rc, "fsharp_rotate")
         return Qo, Ko
 
-    @staticmethod
-    def _cross_check(Q, K, V, key_len, key_mask):
-        """The sizes (B, H, Hk, Lq, Lk, d, dv) and the mask's stride of a cross attention, its tensors checked."""
+    def _cross_check(self, Q, K, V, key_len, key_mask):
+        """The sizes (B, H, Hk, Lq, Lk, d, dv), the lengths' and the mask's address and the mask's stride of a cross attention,
+        its tensors checked."""
+        here, t = self.device, Q.dtype
+        if Q.get_device() != here or K.get_device() != here or V.get_device() != here:
+            self._mine(Q=Q, K=K, V=V)
         B, H, Lq, d = Q.shape
-        if K.dim() != 4 or V.dim() != 4 or K.shape[0] != B or K.shape[3] != d or V.shape[:3] != K.shape[:3] \
-                or K.dtype != Q.dtype or V.dtype != Q.dtype:
+        Bk, Hk, Lk, dk = K.shape
+        Bv, Hv, Lv, dv = V.shape
+        if Bk != B or Bv != B or dk != d or Hv != Hk or Lv != Lk or K.dtype != t or V.dtype != t:
             raise ValueError(f"Q {tuple(Q.shape)} {Q.dtype}, K {tuple(K.shape)} {K.dtype}, V {tuple(V.shape)} {V.dtype}: expected "
                              "[B,H,Lq,d], [B,Hk,Lk,d], [B,Hk,Lk,dv] of one type")
-        _, Hk, Lk, dv = V.shape
-        if key_len is not None and (key_len.dtype != torch.int32 or tuple(key_len.shape) != (B,) or not key_len.is_contiguous()):
-            raise ValueError("key_len: expected a contiguous int32 [B] tensor")
+        len_at = mask_at = None
         mask_stride = 0
+        if key_len is not None:
+            self._mine(key_len=key_len)
+            if key_len.dtype != torch.int32 or tuple(key_len.shape) != (B,) or not key_len.is_contiguous():
+                raise ValueError("key_len: expected a contiguous int32 [B] tensor")
+            len_at = key_len.data_ptr()
         if key_mask is not None:
+            self._mine(key_mask=key_mask)
             if key_mask.dtype not in (torch.bool, torch.uint8) or tuple(key_mask.shape) not in ((B, Lk), (Lk,)) \
                     or (Lk > 1 and key_mask.stride(-1) != 1):
                 raise ValueError("key_mask: expected bool or uint8 [B, Lk] or [Lk] whose last dimension is contiguous")
-            mask_stride = key_mask.stride(0) if key_mask.dim() == 2 else 0
-        return (B, H, Hk, Lq, Lk, d, dv), mask_stride
+            mask_at, mask_stride = key_mask.data_ptr(), key_mask.stride(0) if key_mask.dim() == 2 else 0
+        return (B, H, Hk, Lq, Lk, d, dv), len_at, mask_at, mask_stride
 
     def _cross_scratch(self, dims, dtype, backward, device):
         """The call's scratch: a tensor of its own each time, so that the allocator orders its reuse on the stream and a
@@ -472,23 +485,22 @@ class Context:
         """Exact softmax attention of Q [B,H,Lq,d] to K [B,Hk,Lk,d], V [B,Hk,Lk,dv]: Y, or (Y, lse [B,H,Lq] float32) with
         want_lse.  scale: d^-1/2 if None.  key_len: int32 [B].  key_mask: bool or uint8 [B,Lk] or [Lk], true where a key
         is seen."""
-        self._mine(Q=Q, K=K, V=V, key_len=key_len, key_mask=key_mask, out=out)
         dt = _dtype_code(Q)
-        sizes, mask_stride = self._cross_check(Q, K, V, key_len, key_mask)
+        sizes, len_at, mask_at, mask_stride = self._cross_check(Q, K, V, key_len, key_mask)
         B, H, _, Lq, _, d, dv = sizes
-        device = Q.device
         if out is None:
-            out = torch.empty((B, H, Lq, dv), dtype=Q.dtype, device=device)
+            out, so = Q.new_empty((B, H, Lq, dv)), (H * Lq * dv, Lq * dv, dv)
         else:
+            self._mine(out=out)
             if tuple(out.shape) != (B, H, Lq, dv) or out.dtype != Q.dtype:
                 raise ValueError(f"out: expected {(B, H, Lq, dv)} of {Q.dtype}")
             _check_written("out", out)
-        (Q, sq), (K, sk), (V, sv) = _place(Q), _place(K), _place(V)
-        lse = torch.empty((B, H, Lq), dtype=torch.float32, device=device) if want_lse else None
-        dims = _CROSS_DIMS.pack(*sizes, *sq, *sk, *sv, *_written_place(out), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, mask_stride)
-        scratch, at, n = self._cross_scratch(dims, dt, 0, device)
-        rc = self.lib.fsharp_cross_attend(self._h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), None if key_len is None else key_len.data_ptr(),
-                                          None if key_mask is None else key_mask.data_ptr(), dims, dt, d ** -0.5 if scale is None else scale,
+            so = _written_place(out)
+        (Q, sq, q_at), (K, sk, k_at), (V, sv, v_at) = _place(Q), _place(K), _place(V)
+        lse = Q.new_empty((B, H, Lq), dtype=torch.float32) if want_lse else None
+        dims = _CROSS_DIMS.pack(*sizes, *sq, *sk, *sv, *so, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, mask_stride)
+        scratch, at, n = self._cross_scratch(dims, dt, 0, Q.device)
+        rc = self.lib.fsharp_cross_attend(self._h, q_at, k_at, v_at, len_at, mask_at, dims, dt, d ** -0.5 if scale is None else scale,
                                           out.data_ptr(), lse.data_ptr() if want_lse else None, at, n)
         if rc:
             raise FsharpError(rc, "fsharp_cross_attend")
@@ -497,9 +509,9 @@ class Context:
     def fsharp_cross_attend_backward(self, Q, K, V, Y, lse, dY, scale=None, key_len=None, key_mask=None):
         """(dQ, dK, dV) for the cotangent dY of fsharp_cross_attend's Y, with the Y and lse of that call; each gradient is a
         new tensor with its tensor's shape and, where those give every value a place of its own, its order of dimensions."""
-        self._mine(Q=Q, K=K, V=V, Y=Y, lse=lse, dY=dY, key_len=key_len, key_mask=key_mask)
         dt = _dtype_code(Q)
-        sizes, mask_stride = self._cross_check(Q, K, V, key_len, key_mask)
+        sizes, len_at, mask_at, mask_stride = self._cross_check(Q, K, V, key_len, key_mask)
+        self._mine(Y=Y, lse=lse, dY=dY)
         B, H, _, Lq, _, d, dv = sizes
         for name, t in (("Y", Y), ("dY", dY)):
             if tuple(t.shape) != (B, H, Lq, dv) or t.dtype != Q.dtype:
@@ -507,14 +519,13 @@ class Context:
         if tuple(lse.shape) != (B, H, Lq) or lse.dtype != torch.float32 or not lse.is_contiguous():
             raise ValueError(f"lse: expected a contiguous float32 tensor of shape {(B, H, Lq)}")
         dQ, dK, dV = torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V)      # (permuted like a dense tensor, else dense)
-        (Q, sq), (K, sk), (V, sv), (Y, sy), (dY, sg) = _place(Q), _place(K), _place(V), _place(Y), _place(dY)
+        (Q, sq, q_at), (K, sk, k_at), (V, sv, v_at), (Y, sy, y_at), (dY, sg, g_at) = (_place(t) for t in (Q, K, V, Y, dY))
         dims = _CROSS_DIMS.pack(*sizes, *sq, *sk, *sv, *sy, *sg, *_written_place(dQ), *_written_place(dK), *_written_place(dV),
                                 mask_stride)
         scratch, at, n = self._cross_scratch(dims, dt, 1, Q.device)
         rc = self.lib.fsharp_cross_attend_backward(
-            self._h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), Y.data_ptr(), lse.data_ptr(), dY.data_ptr(),
-            None if key_len is None else key_len.data_ptr(), None if key_mask is None else key_mask.data_ptr(), dims, dt,
-            d ** -0.5 if scale is None else scale, dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), at, n)
+            self._h, q_at, k_at, v_at, y_at, lse.data_ptr(), g_at, len_at, mask_at, dims, dt, d ** -0.5 if scale is None else scale,
+            dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), at, n)
         if rc:
             raise FsharpError(rc, "fsharp_cross_attend_backward")
         return dQ, dK, dV
