@@ -70,12 +70,36 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   const bool both = R - r0 > TILE;                     // each warpgroup has rows of its own
   const int items = both ? 2 * nt : nt;                // item i: warpgroup i & 1, tile i / 2 or i
 
-  if (threadIdx.x == 0) {
+  const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;      // panels of 64 columns
+  // (a stride of zero, one entry for all, is a dimension of size one in the tensor map)
+  const int kh = a.ak.sh ? hk : 0, kb = a.ak.sb ? b : 0, vh = a.av.sh ? hk : 0, vb = a.av.sb ? b : 0;
+  auto load = [&](int i) {                             // the i-th tile of the ring: K and V in turn
+    const int s = i % Sm::NS, tok = (t0 + i / 2) * KT, panels = i & 1 ? vp : kp;
+    uint8_t* base = sm + Sm::RING + s * Sm::SLOT;
+    mbar_expect_tx(&misc->full[s], panels * Sm::PANEL);
+    for (int p = 0; p < panels; p++)
+      tma_load_4d(base + p * Sm::PANEL, i & 1 ? &tmV : &tmK, &misc->full[s], p * 64, tok, i & 1 ? vh : kh, i & 1 ? vb : kb);
+  };
+  if (threadIdx.x == CXW_TMA * 32) {                   // (the thread that issues the copies)
     for (int i = 0; i < Sm::NS; i++) { mbar_init(&misc->full[i], 1); mbar_init(&misc->empty[i], 1); }
     for (int w = 0; w < 2; w++) { mbar_init(&misc->s_full[w], 1); mbar_init(&misc->s_free[w], 4); mbar_init(&misc->p_ready[w], 4); mbar_init(&misc->o_full[w], 1); }
     mbar_init(&misc->q_ready, CX_WARPS);
     misc->abort_flag = 0;
     fence_barrier_init();
+    fence_proxy_async_smem();
+    for (int i = 0; i < Sm::NS && i < 2 * nt; i++) load(i);      // the ring's first round, while the others make ready
+  }
+  if (warp < CX_WARPS) {
+    // the block's rows of Q into shared memory, rows and columns that there are none of as zeros
+    constexpr int CH = D / 8;
+    const int rows = both ? 256 : 128;
+    const __nv_bfloat16* Q = static_cast<const __nv_bfloat16*>(a.Q) + b * a.aq.sb;
+    for (int i = threadIdx.x; i < rows * CH; i += 256) {
+      const int rr = i / CH, ch = i % CH, r = r0 + rr;
+      const bool some = r < R && ch * 8 < a.d;
+      copy16(sm + Sm::Q + (rr >> 7) * Sm::QT + (ch >> 3) * TILE_BYTES + sw128_offset(rr & 127, (ch & 7) * 8),
+             Q + (some ? (int64_t)(hk * a.g + r / a.Lq) * a.aq.sh + (int64_t)(r % a.Lq) * a.aq.sl + ch * 8 : 0), some);
+    }
   }
   if (warp == CXW_MMA) {
     tmem_alloc(&misc->tmem_base, CX_TMEM);
@@ -85,24 +109,14 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   __syncthreads();
   tcgen05_fence_after();
   const uint32_t tmem = misc->tmem_base;
-  const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;      // panels of 64 columns
 
   if (warp >= CX_WARPS) regs_release<CX_REGS_REST>();
   if (warp == CXW_TMA) {
     if (lane == 0) {
-      prefetch_tmap(&tmK); prefetch_tmap(&tmV);
-      bool ok = true;
-      int issued = 0;
-      // (a stride of zero, one entry for all, is a dimension of size one in the tensor map)
-      const int ch[2] = {a.ak.sh ? hk : 0, a.av.sh ? hk : 0}, cb[2] = {a.ak.sb ? b : 0, a.av.sb ? b : 0};
-      for (; issued < 2 * nt && ok; issued++) {
-        const int s = issued % Sm::NS, tok = (t0 + issued / 2) * KT;
-        if (!mbar_wait(&misc->empty[s], ((issued / Sm::NS) & 1) ^ 1, abortp, status)) { ok = false; break; }
-        uint8_t* base = sm + Sm::RING + s * Sm::SLOT;
-        const CUtensorMap* map = issued & 1 ? &tmV : &tmK;
-        const int panels = issued & 1 ? vp : kp;
-        mbar_expect_tx(&misc->full[s], panels * Sm::PANEL);
-        for (int p = 0; p < panels; p++) tma_load_4d(base + p * Sm::PANEL, map, &misc->full[s], p * 64, tok, ch[issued & 1], cb[issued & 1]);
+      int issued = min(Sm::NS, 2 * nt);
+      for (; issued < 2 * nt; issued++) {
+        if (!mbar_wait(&misc->empty[issued % Sm::NS], ((issued / Sm::NS) & 1) ^ 1, abortp, status)) break;
+        load(issued);
       }
       // nothing of this block may still be in flight when it exits: no copy, and no arrival of a product's completion
       for (int i = max(0, issued - Sm::NS); i < issued; i++) {
@@ -164,21 +178,9 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   } else if (warp < CX_WARPS) {
     regs_acquire<CX_REGS_ROWS>();
     const int w = warp >> 2, row = (warp & 3) * 32 + lane;
-    {
-      // the block's rows of Q into shared memory, rows and columns that there are none of as zeros
-      constexpr int CH = D / 8;
-      const int rows = both ? 256 : 128;
-      const __nv_bfloat16* Q = static_cast<const __nv_bfloat16*>(a.Q) + b * a.aq.sb;
-      for (int i = threadIdx.x; i < rows * CH; i += 256) {
-        const int rr = i / CH, ch = i % CH, r = r0 + rr;
-        const bool some = r < R && ch * 8 < a.d;
-        copy16(sm + Sm::Q + (rr >> 7) * Sm::QT + (ch >> 3) * TILE_BYTES + sw128_offset(rr & 127, (ch & 7) * 8),
-               Q + (some ? (int64_t)(hk * a.g + r / a.Lq) * a.aq.sh + (int64_t)(r % a.Lq) * a.aq.sl + ch * 8 : 0), some);
-      }
-      copies_done();
-      fence_proxy_async_smem();
-      mbar_arrive_warp(&misc->q_ready, lane);
-    }
+    copies_done();
+    fence_proxy_async_smem();
+    mbar_arrive_warp(&misc->q_ready, lane);
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), tS = lanes + w * Sm::GROUP + Sm::S, tP = lanes + w * Sm::GROUP + Sm::P, tO = lanes + w * Sm::GROUP + Sm::O;
     const int first = r0 + (both ? w * TILE : 0), r = first + row;      // this thread's row
     const bool idle = first + (warp & 3) * 32 >= R;                     // no row of this warp exists

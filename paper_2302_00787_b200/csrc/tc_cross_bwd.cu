@@ -72,9 +72,25 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   // row tiles: those of the first query head of the group, of the second, ...
   const int per = (a.Lq + T - 1) / T;
   const int64_t tiles = j0 < n ? (int64_t)a.g * per : 0;
+  const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;      // panels of 64 columns
   const int t0 = (int)(tiles * piece / gr.kv_pieces), items = (int)(tiles * (piece + 1) / gr.kv_pieces) - t0;
 
-  if (threadIdx.x == 0) {
+  // 16 values of key j0 + row of dV (w = 0) or dK, or of a piece's sums of them
+  auto store = [&](int w, int row, int q, const float (&x)[16]) {
+    const int j = j0 + row;
+    const TensorAddr to = w ? gr.adk : gr.adv;
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(w ? gr.dK : gr.dV) + b * to.sb + hk * to.sh + j * to.sl + q;
+    float* part = gr.pkv + (((int64_t)piece * a.B * a.Hk + unit) * a.Lk + j) * (a.d + a.dv) + (w ? 0 : a.d) + q;
+    store_row(j < a.Lk, x, gr.pkv ? part : nullptr, out);
+  };
+  if (items == 0) {                                    // keys behind the sequence's end (or a piece without rows)
+    const float none[16] = {};
+    if (threadIdx.x < 256)
+      for (int w = threadIdx.x >> 7, q = 0; q < (w ? a.d : a.dv); q += 16) store(w, threadIdx.x & 127, q, none);
+    return;
+  }
+
+  if (threadIdx.x == CGW_TMA * 32) {                   // (the thread that issues the copies)
     for (int i = 0; i < Sm::NS; i++) { mbar_init(&misc->q_full[i], 1); mbar_init(&misc->q_empty[i], 1); mbar_init(&misc->g_full[i], 1); mbar_init(&misc->g_empty[i], 1); }
     mbar_init(&misc->s_full, 1);
     mbar_init(&misc->dp_full, 1);
@@ -84,6 +100,11 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     mbar_init(&misc->done, 1);
     misc->abort_flag = 0;
     fence_barrier_init();
+    fence_proxy_async_smem();
+    // the block's keys, while the others make ready
+    mbar_expect_tx(&misc->kv_full, (kp + vp) * TILE_BYTES);
+    for (int p = 0; p < kp; p++) tma_load_4d(sm + Sm::K + p * TILE_BYTES, &tmK, &misc->kv_full, p * 64, j0, a.ak.sh ? hk : 0, a.ak.sb ? b : 0);
+    for (int p = 0; p < vp; p++) tma_load_4d(sm + Sm::V + p * TILE_BYTES, &tmV, &misc->kv_full, p * 64, j0, a.av.sh ? hk : 0, a.av.sb ? b : 0);
   }
   if (warp == CGW_MMA) {
     tmem_alloc(&misc->tmem_base, Sm::COLUMNS);
@@ -93,15 +114,10 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   __syncthreads();
   tcgen05_fence_after();
   const uint32_t tmem = misc->tmem_base;
-  const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;
 
   if (warp >= CG_WARPS) regs_release<(Sm::BLOCKS == 2 ? CG_REGS_REST2 : CG_REGS_REST)>();
   if (warp == CGW_TMA) {
-    if (lane == 0 && items > 0) {
-      prefetch_tmap(&tmQ); prefetch_tmap(&tmG); prefetch_tmap(&tmK); prefetch_tmap(&tmV);
-      mbar_expect_tx(&misc->kv_full, (kp + vp) * TILE_BYTES);
-      for (int p = 0; p < kp; p++) tma_load_4d(sm + Sm::K + p * TILE_BYTES, &tmK, &misc->kv_full, p * 64, j0, a.ak.sh ? hk : 0, a.ak.sb ? b : 0);
-      for (int p = 0; p < vp; p++) tma_load_4d(sm + Sm::V + p * TILE_BYTES, &tmV, &misc->kv_full, p * 64, j0, a.av.sh ? hk : 0, a.av.sb ? b : 0);
+    if (lane == 0) {
       int i = 0;
       for (; i < items; i++) {
         const int s = i % Sm::NS, h = hk * a.g + (t0 + i) / per, t = (t0 + i) % per;
@@ -167,7 +183,7 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       __syncwarp();
       return true;
     };
-    bool ok = items > 0 && wait(&misc->kv_full, 0) && issue_s(0) && issue_dp(0);
+    bool ok = wait(&misc->kv_full, 0) && issue_s(0) && issue_dp(0);
     for (int i = 0; i < items && ok; i++) {
       const int s = i % Sm::NS;
       if (!(ok = wait(&misc->p_ready, i & 1))) break;
@@ -253,26 +269,21 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       tcgen05_fence_before();
       mbar_arrive_warp(&misc->ds_ready, lane);
     }
-    if (ok && items > 0) ok = __all_sync(0xffffffffu, mbar_wait(&misc->done, 0, abortp, status, false));
+    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&misc->done, 0, abortp, status, false));
     tcgen05_fence_after();
     if (ok) {
       // the first warpgroup writes dV, the second dK
       const int j = j0 + row, width = w ? a.d : a.dv;
       const bool on = cross_seen(a, b, j, n);
       const float f = w ? a.scale : 1.f;
-      const TensorAddr to = w ? gr.adk : gr.adv;
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(w ? gr.dK : gr.dV) + b * to.sb + hk * to.sh + j * to.sl;
-      float* part = gr.pkv + (((int64_t)piece * a.B * a.Hk + unit) * a.Lk + j) * (a.d + a.dv) + (w ? 0 : a.d);
       for (int q = 0; q < width; q += 16) {
-        uint32_t t[16] = {};
-        if (items > 0) {
-          tmem_ld16(lanes + (w ? Sm::DK : Sm::DV) + q, t);
-          tmem_wait_ld();
-        }
+        uint32_t t[16];
+        tmem_ld16(lanes + (w ? Sm::DK : Sm::DV) + q, t);
+        tmem_wait_ld();
         float x[16];
 #pragma unroll
         for (int k = 0; k < 16; k++) x[k] = on ? __uint_as_float(t[k]) * f : 0.f;
-        store_row(j < a.Lk, x, gr.pkv ? part + q : nullptr, out + q);
+        store(w, row, q, x);
       }
     }
   }
@@ -321,12 +332,35 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   const bool both = R - r0 > TILE;                     // each warpgroup has rows of its own
   const int items = both ? 2 * nt : nt;                // item i: warpgroup i & 1, tile i / 2 or i
 
-  if (threadIdx.x == 0) {
+  const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;      // panels of 64 columns
+  auto load = [&](int i) {                             // tile i of K and of V
+    const int s = i % Sm::NS, tok = (t0 + i) * HALF;
+    uint8_t* base = sm + Sm::RING + s * Sm::STAGE;
+    mbar_expect_tx(&misc->full[s], (kp + vp) * HALF_BYTES);
+    for (int p = 0; p < kp; p++) tma_load_4d(base + p * HALF_BYTES, &tmK, &misc->full[s], p * 64, tok, a.ak.sh ? hk : 0, a.ak.sb ? b : 0);
+    for (int p = 0; p < vp; p++) tma_load_4d(base + Sm::SLOT + p * HALF_BYTES, &tmV, &misc->full[s], p * 64, tok, a.av.sh ? hk : 0, a.av.sb ? b : 0);
+  };
+  if (threadIdx.x == CGW_TMA * 32) {                   // (the thread that issues the copies)
     for (int i = 0; i < Sm::NS; i++) { mbar_init(&misc->full[i], 1); mbar_init(&misc->empty[i], 1); }
     for (int w = 0; w < 2; w++) { mbar_init(&misc->sp_full[w], 1); mbar_init(&misc->ready[w], 4); mbar_init(&misc->done[w], 1); }
     mbar_init(&misc->q_ready, CG_WARPS);
     misc->abort_flag = 0;
     fence_barrier_init();
+    fence_proxy_async_smem();
+    for (int i = 0; i < Sm::NS && i < nt; i++) load(i);      // the ring's first round, while the others make ready
+  }
+  if (warp < CG_WARPS) {
+    // the block's rows of Q and dY into shared memory, rows and columns that there are none of as zeros
+    constexpr int CH = D / 8;
+    const int rows = both ? 256 : 128;
+    for (int i = threadIdx.x; i < 2 * rows * CH; i += 256) {
+      const int which = i >= rows * CH, k = i - which * rows * CH, rr = k / CH, ch = k % CH, r = r0 + rr;
+      const TensorAddr t = which ? gr.ady : a.aq;
+      const __nv_bfloat16* X = static_cast<const __nv_bfloat16*>(which ? gr.dY : a.Q) + b * t.sb;
+      const bool some = r < R && ch * 8 < (which ? a.dv : a.d);
+      copy16(sm + (which ? Sm::G : Sm::Q) + (rr >> 7) * Sm::BIG + (ch >> 3) * TILE_BYTES + sw128_offset(rr & 127, (ch & 7) * 8),
+             X + (some ? (int64_t)(hk * a.g + r / a.Lq) * t.sh + (int64_t)(r % a.Lq) * t.sl + ch * 8 : 0), some);
+    }
   }
   if (warp == CGW_MMA) {
     tmem_alloc(&misc->tmem_base, CG_DQ_TMEM);
@@ -336,20 +370,14 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   __syncthreads();
   tcgen05_fence_after();
   const uint32_t tmem = misc->tmem_base;
-  const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;
 
   if (warp >= CG_WARPS) regs_release<CG_REGS_REST>();
   if (warp == CGW_TMA) {
     if (lane == 0) {
-      prefetch_tmap(&tmK); prefetch_tmap(&tmV);
-      int i = 0;
+      int i = min(Sm::NS, nt);
       for (; i < nt; i++) {
-        const int s = i % Sm::NS, tok = (t0 + i) * HALF;
-        if (!mbar_wait(&misc->empty[s], ((i / Sm::NS) & 1) ^ 1, abortp, status)) break;
-        uint8_t* base = sm + Sm::RING + s * Sm::STAGE;
-        mbar_expect_tx(&misc->full[s], (kp + vp) * HALF_BYTES);
-        for (int p = 0; p < kp; p++) tma_load_4d(base + p * HALF_BYTES, &tmK, &misc->full[s], p * 64, tok, a.ak.sh ? hk : 0, a.ak.sb ? b : 0);
-        for (int p = 0; p < vp; p++) tma_load_4d(base + Sm::SLOT + p * HALF_BYTES, &tmV, &misc->full[s], p * 64, tok, a.av.sh ? hk : 0, a.av.sb ? b : 0);
+        if (!mbar_wait(&misc->empty[i % Sm::NS], ((i / Sm::NS) & 1) ^ 1, abortp, status)) break;
+        load(i);
       }
       // nothing of this block may still be in flight when it exits: no copy, and no arrival of a product's completion
       for (int k = max(0, i - Sm::NS); k < i; k++) {
@@ -407,22 +435,9 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   } else if (warp < CG_WARPS) {
     regs_acquire<CG_REGS_ROWS>();
     const int w = warp >> 2, row = (warp & 3) * 32 + lane;
-    {
-      // the block's rows of Q and dY into shared memory, rows and columns that there are none of as zeros
-      constexpr int CH = D / 8;
-      const int rows = both ? 256 : 128;
-      for (int i = threadIdx.x; i < 2 * rows * CH; i += 256) {
-        const int which = i >= rows * CH, k = i - which * rows * CH, rr = k / CH, ch = k % CH, r = r0 + rr;
-        const TensorAddr t = which ? gr.ady : a.aq;
-        const __nv_bfloat16* X = static_cast<const __nv_bfloat16*>(which ? gr.dY : a.Q) + b * t.sb;
-        const bool some = r < R && ch * 8 < (which ? a.dv : a.d);
-        copy16(sm + (which ? Sm::G : Sm::Q) + (rr >> 7) * Sm::BIG + (ch >> 3) * TILE_BYTES + sw128_offset(rr & 127, (ch & 7) * 8),
-               X + (some ? (int64_t)(hk * a.g + r / a.Lq) * t.sh + (int64_t)(r % a.Lq) * t.sl + ch * 8 : 0), some);
-      }
-      copies_done();
-      fence_proxy_async_smem();
-      mbar_arrive_warp(&misc->q_ready, lane);
-    }
+    copies_done();
+    fence_proxy_async_smem();
+    mbar_arrive_warp(&misc->q_ready, lane);
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), tS = lanes + w * 128, tP = tS + 64, tQ = lanes + CG_DQ_SUM + w * 128;
     const int first = r0 + (both ? w * TILE : 0), r = first + row;
     const bool idle = first + (warp & 3) * 32 >= R;
