@@ -178,6 +178,7 @@ CrossArgs args_of(const fsharp_cross_dims* dm, const void* Q, const void* K, con
   a.key_len = key_len; a.key_mask = key_mask; a.mask_stride = dm->mask_stride;
   a.B = dm->B; a.H = dm->H; a.Hk = dm->Hk; a.g = dm->H / dm->Hk; a.Lq = dm->Lq; a.Lk = dm->Lk; a.d = dm->d; a.dv = dm->dv;
   a.scale = scale;
+  a.ranked = 0;
   return a;
 }
 

@@ -13,6 +13,7 @@ struct CrossArgs {
   int64_t mask_stride;
   int B, H, Hk, g, Lq, Lk, d, dv;
   float scale;             // of the scores; kernels multiply by log2(e) where they need it
+  int ranked;              // blocks take the units in the order of their sequences' lengths (cross_rank)
 };
 
 // The keys of sequence b: no more than this many.
@@ -21,6 +22,37 @@ __device__ __forceinline__ int cross_keys(const CrossArgs& a, int b) {
 }
 __device__ __forceinline__ bool cross_seen(const CrossArgs& a, int b, int j, int n) {
   return j < n && (!a.key_mask || a.key_mask[b * a.mask_stride + j] != 0);
+}
+
+// The batch's sequences from the longest to the shortest, into order[B]: a block's time goes with its sequence's length; with the
+// longest first, what runs alone at the end is short.  room: B ints of shared memory, free again when the call returns.  All
+// threads of the block.
+constexpr int CROSS_RANKED = 256;      // most sequences that are ranked
+__device__ __forceinline__ void cross_rank(const CrossArgs& a, int* room, uint8_t* order) {
+  const int t = threadIdx.x;
+  if (t < a.B) room[t] = cross_keys(a, t);
+  __syncthreads();
+  if (t < a.B) {
+    const int mine = room[t];
+    int rank = 0;
+    for (int b = 0; b < a.B; b++) rank += room[b] > mine || (room[b] == mine && b < t);
+    order[rank] = (uint8_t)t;
+  }
+  __syncthreads();
+}
+// The unit of a block of a grid with a unit per blockIdx.y.
+__device__ __forceinline__ int cross_unit(const CrossArgs& a, int* room) {
+  const int u = blockIdx.y;
+  if (!a.ranked) return u;
+  uint8_t* order = reinterpret_cast<uint8_t*>(room + CROSS_RANKED);
+  cross_rank(a, room, order);
+  const int b = order[u / a.Hk];
+  __syncthreads();
+  return b * a.Hk + u % a.Hk;
+}
+// Whether it is worth it: lengths differ, and the blocks do not all run at once.
+static inline int cross_ranked(const fsharp_ctx* ctx, const CrossArgs& a, int64_t blocks) {
+  return a.key_len && a.B > 1 && a.B <= CROSS_RANKED && blocks > ctx->sm_count;
 }
 
 // Pieces of a unit's keys (or rows) that blocks of their own take, so that few units fill the GPU: partial results go to scratch.

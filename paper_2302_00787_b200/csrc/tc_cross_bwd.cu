@@ -325,7 +325,7 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   DqMs* misc = reinterpret_cast<DqMs*>(sm + Sm::MISC);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abortp = &misc->abort_flag;
-  const int unit = blockIdx.y, piece = blockIdx.x % gr.q_pieces, r0 = (int)(blockIdx.x / gr.q_pieces) * 256;
+  const int unit = cross_unit(a, reinterpret_cast<int*>(sm + Sm::Q)), piece = blockIdx.x % gr.q_pieces, r0 = (int)(blockIdx.x / gr.q_pieces) * 256;
   const int b = unit / a.Hk, hk = unit % a.Hk, R = a.g * a.Lq;
   const int n = cross_keys(a, b), tiles = (n + HALF - 1) / HALF;
   const int t0 = (int)((int64_t)tiles * piece / gr.q_pieces), nt = (int)((int64_t)tiles * (piece + 1) / gr.q_pieces) - t0;
@@ -559,8 +559,10 @@ int launch(fsharp_ctx* ctx, const CrossArgs& a, const CrossGrad& gr) {
   tc_cross_dkv_kernel<D><<<dim3((unsigned)gk, (unsigned)(a.B * a.Hk)), CG_T, KvSm<D>::TOTAL + 1024, ctx->stream>>>(tmQ, tmG, tmK, tmV, a, gr, ctx->d_status);
   FS_TIME_END(ctx);
   FS_LAUNCH_CHECK(ctx);
+  CrossArgs aq = a;
+  aq.ranked = cross_ranked(ctx, a, gq * a.B * a.Hk);
   FS_TIME_BEGIN(ctx, FS_K_TC_CROSS_DQ);
-  tc_cross_dq_kernel<D><<<dim3((unsigned)gq, (unsigned)(a.B * a.Hk)), CG_T, DqSm<D>::TOTAL + 1024, ctx->stream>>>(tmKt, tmVt, a, gr, ctx->d_status);
+  tc_cross_dq_kernel<D><<<dim3((unsigned)gq, (unsigned)(a.B * a.Hk)), CG_T, DqSm<D>::TOTAL + 1024, ctx->stream>>>(tmKt, tmVt, aq, gr, ctx->d_status);
   FS_TIME_END(ctx);
   FS_LAUNCH_CHECK(ctx);
   return FSHARP_OK;

@@ -152,7 +152,7 @@ tc_cross_f32_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   FwMs* misc = reinterpret_cast<FwMs*>(sm + Sm::MISC);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abortp = &misc->abort_flag;
-  const int unit = blockIdx.y, piece = blockIdx.x % part.pieces, r0 = (int)(blockIdx.x / part.pieces) * 256;
+  const int unit = cross_unit(a, reinterpret_cast<int*>(sm + Sm::Q)), piece = blockIdx.x % part.pieces, r0 = (int)(blockIdx.x / part.pieces) * 256;
   const int b = unit / a.Hk, hk = unit % a.Hk, R = a.g * a.Lq;
   const int n = cross_keys(a, b), tiles = (n + KT - 1) / KT;
   const int t0 = (int)((int64_t)tiles * piece / part.pieces), nt = (int)((int64_t)tiles * (piece + 1) / part.pieces) - t0;
@@ -623,7 +623,7 @@ tc_cross_f32_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
   FqMs* misc = reinterpret_cast<FqMs*>(sm + Sm::MISC);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abortp = &misc->abort_flag;
-  const int unit = blockIdx.y, piece = blockIdx.x % gr.q_pieces, r0 = (int)(blockIdx.x / gr.q_pieces) * TILE;
+  const int unit = cross_unit(a, reinterpret_cast<int*>(sm + Sm::Q)), piece = blockIdx.x % gr.q_pieces, r0 = (int)(blockIdx.x / gr.q_pieces) * TILE;
   const int b = unit / a.Hk, hk = unit % a.Hk, R = a.g * a.Lq;
   const int n = cross_keys(a, b), tiles = (n + KT - 1) / KT;
   const int t0 = (int)((int64_t)tiles * piece / gr.q_pieces), nt = (int)((int64_t)tiles * (piece + 1) / gr.q_pieces) - t0;
@@ -884,8 +884,10 @@ int fs_tc_cross_f32(fsharp_ctx* ctx, const CrossArgs& a, void* Y, TensorAddr ay,
   const int64_t gx = ((int64_t)a.g * a.Lq + 255) / 256 * part.pieces;
   if (gx > 0x7fffffff) return FSHARP_E_SHAPE;
   FS_CUDA_OK(fs_allow_smem(tc_cross_f32_kernel));
+  CrossArgs af = a;
+  af.ranked = cross_ranked(ctx, a, gx * a.B * a.Hk);
   FS_TIME_BEGIN(ctx, FS_K_TC_CROSS);
-  tc_cross_f32_kernel<<<dim3((unsigned)gx, (unsigned)(a.B * a.Hk)), CF_T, FwSm::TOTAL + 1024, ctx->stream>>>(tmK, tmV, a, static_cast<float*>(Y), ay, lse, part, ctx->d_status);
+  tc_cross_f32_kernel<<<dim3((unsigned)gx, (unsigned)(a.B * a.Hk)), CF_T, FwSm::TOTAL + 1024, ctx->stream>>>(tmK, tmV, af, static_cast<float*>(Y), ay, lse, part, ctx->d_status);
   FS_TIME_END(ctx);
   FS_LAUNCH_CHECK(ctx);
   return FSHARP_OK;
@@ -916,8 +918,10 @@ int fs_tc_cross_f32_grad(fsharp_ctx* ctx, const CrossArgs& a, const CrossGrad& g
   tc_cross_f32_dkv_kernel<<<dim3((unsigned)gk, (unsigned)(a.B * a.Hk)), CF_T, FkSm::TOTAL + 1024, ctx->stream>>>(tmQ, tmG, tmK, tmV, a, gr, ctx->d_status);
   FS_TIME_END(ctx);
   FS_LAUNCH_CHECK(ctx);
+  CrossArgs aq = a;
+  aq.ranked = cross_ranked(ctx, a, gq * a.B * a.Hk);
   FS_TIME_BEGIN(ctx, FS_K_TC_CROSS_DQ);
-  tc_cross_f32_dq_kernel<<<dim3((unsigned)gq, (unsigned)(a.B * a.Hk)), CF_T, FqSm::TOTAL + 1024, ctx->stream>>>(tmKt, tmVt, a, gr, ctx->d_status);
+  tc_cross_f32_dq_kernel<<<dim3((unsigned)gq, (unsigned)(a.B * a.Hk)), CF_T, FqSm::TOTAL + 1024, ctx->stream>>>(tmKt, tmVt, aq, gr, ctx->d_status);
   FS_TIME_END(ctx);
   FS_LAUNCH_CHECK(ctx);
   return FSHARP_OK;
