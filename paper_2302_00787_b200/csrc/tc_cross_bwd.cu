@@ -43,23 +43,32 @@ template <int D>
 struct KvSm {
   static constexpr int T = D == 64 ? 64 : 128, BLOCKS = D == 64 ? 2 : 1, PANELS = D / 64, NS = D == 64 ? 4 : 2;      // NS: tiles of Q and of dY in flight
   static constexpr uint32_t PANEL = T * 128, BIG = PANELS * TILE_BYTES, TILE_D = PANELS * PANEL, K = 0, V = BIG, Q = 2 * BIG, G = Q + NS * TILE_D, STAT = G + NS * TILE_D;
-  static constexpr uint32_t MISC = STAT + NS * 8 * T, TOTAL = MISC + 512;
+  static constexpr uint32_t MISC = STAT + NS * 8 * T, TOTAL = MISC + 1536;
   static constexpr uint32_t S = 0, P = T, DV = 2 * T, DK = 2 * T + D, COLUMNS = BLOCKS == 2 ? 256 : 512;
   static_assert(BLOCKS * (TOTAL + 2048) <= 233472, "shared memory budget");
   static_assert(DK + D <= COLUMNS, "tensor memory");
 };
 struct KvMs {
-  uint64_t q_full[4], q_empty[4], g_full[4], g_empty[4], s_full, p_ready, dp_full, ds_ready, kv_full, done;
+  uint64_t q_full[4], q_empty[4], g_full[4], g_empty[4], s_full, p_ready, dp_full, ds_ready, kv_full, kv_empty, done;
   uint32_t tmem_base;
   int abort_flag;
+  int live[CROSS_RANKED + 1];                          // tiles of keys that the sequences before one have
 };
-static_assert(sizeof(KvMs) <= 512, "misc block");
+static_assert(sizeof(KvMs) <= 1536, "misc block");
 
+// One piece of work: 128 keys against a piece of the rows of the query heads that share them.
+struct KvWork {
+  int unit, piece, b, hk, j0, n, t0, items;
+};
+
+// Blocks are persistent and take every gridDim.x-th piece of the work that there is: tiles behind a sequence's end are written with zeros
+// on the way.  The next piece's keys and rows are copied, and its first S^T and dP^T made, while this one's sums go out.  (A block per
+// piece: 17.5 us each for 16 x 12 x 512 x 1500, 11.2 of them at its tiles, and 5 us from one to the next: 117 us.)
 template <int D>
 __global__ void __launch_bounds__(CG_T, KvSm<D>::BLOCKS)
 tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmG, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CrossArgs a, const __grid_constant__ CrossGrad gr,
-                    int* __restrict__ status) {
+                    int key_tiles, int* __restrict__ status) {
   using Sm = KvSm<D>;
   constexpr int T = Sm::T;
   extern __shared__ uint8_t smem_raw[];
@@ -67,77 +76,118 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   KvMs* misc = reinterpret_cast<KvMs*>(sm + Sm::MISC);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abortp = &misc->abort_flag;
-  const int unit = blockIdx.y, piece = blockIdx.x % gr.kv_pieces, j0 = (int)(blockIdx.x / gr.kv_pieces) * TILE;
-  const int b = unit / a.Hk, hk = unit % a.Hk, n = cross_keys(a, b);
-  // row tiles: those of the first query head of the group, of the second, ...
-  const int per = (a.Lq + T - 1) / T;
-  const int64_t tiles = j0 < n ? (int64_t)a.g * per : 0;
-  const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;      // panels of 64 columns
-  const int t0 = (int)(tiles * piece / gr.kv_pieces), items = (int)(tiles * (piece + 1) / gr.kv_pieces) - t0;
+  const int per = (a.Lq + T - 1) / T;                  // row tiles: those of the first query head of the group, of the second, ...
+  const int row_tiles = a.g * per;
+  // Without lengths, or with more of them than are listed, every tile counts as live (the rows of a tile that is not come to nothing).
+  const bool listed = a.key_len != nullptr && a.B <= CROSS_RANKED;
 
-  // 16 values of key j0 + row of dV (w = 0) or dK, or of a piece's sums of them
-  auto store = [&](int w, int row, int q, const float (&x)[16]) {
-    const int j = j0 + row;
-    const TensorAddr to = w ? gr.adk : gr.adv;
-    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(w ? gr.dK : gr.dV) + b * to.sb + hk * to.sh + j * to.sl + q;
-    float* part = gr.pkv + (((int64_t)piece * a.B * a.Hk + unit) * a.Lk + j) * (a.d + a.dv) + (w ? 0 : a.d) + q;
-    store_row(j < a.Lk, x, gr.pkv ? part : nullptr, out);
-  };
-  if (items == 0) {                                    // keys behind the sequence's end (or a piece without rows)
-    const float none[16] = {};
-    if (threadIdx.x < 256)
-      for (int w = threadIdx.x >> 7, q = 0; q < (w ? a.d : a.dv); q += 16) store(w, threadIdx.x & 127, q, none);
-    return;
-  }
-
-  if (threadIdx.x == CGW_TMA * 32) {                   // (the thread that issues the copies)
+  if (threadIdx.x == 0) {
     for (int i = 0; i < Sm::NS; i++) { mbar_init(&misc->q_full[i], 1); mbar_init(&misc->q_empty[i], 1); mbar_init(&misc->g_full[i], 1); mbar_init(&misc->g_empty[i], 1); }
     mbar_init(&misc->s_full, 1);
     mbar_init(&misc->dp_full, 1);
     mbar_init(&misc->p_ready, CG_WARPS);
     mbar_init(&misc->ds_ready, CG_WARPS);
     mbar_init(&misc->kv_full, 1);
+    mbar_init(&misc->kv_empty, 1);
     mbar_init(&misc->done, 1);
     misc->abort_flag = 0;
     fence_barrier_init();
-    fence_proxy_async_smem();
-    // the block's keys, while the others make ready
-    mbar_expect_tx(&misc->kv_full, (kp + vp) * TILE_BYTES);
-    for (int p = 0; p < kp; p++) tma_load_4d(sm + Sm::K + p * TILE_BYTES, &tmK, &misc->kv_full, p * 64, j0, a.ak.sh ? hk : 0, a.ak.sb ? b : 0);
-    for (int p = 0; p < vp; p++) tma_load_4d(sm + Sm::V + p * TILE_BYTES, &tmV, &misc->kv_full, p * 64, j0, a.av.sh ? hk : 0, a.av.sb ? b : 0);
   }
   if (warp == CGW_MMA) {
     tmem_alloc(&misc->tmem_base, Sm::COLUMNS);
     tmem_relinquish();
   }
+  if (listed && warp == 0) {
+    // live tiles of the sequences before each
+    int before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+      const int b = b0 + lane, own = b < a.B ? (cross_keys(a, b) + TILE - 1) / TILE : 0;
+      int sum = own;
+#pragma unroll
+      for (int k = 1; k < 32; k <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, sum, k);
+        if (lane >= k) sum += x;
+      }
+      if (b < a.B) misc->live[b + 1] = before + sum;
+      before += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    if (lane == 0) misc->live[0] = 0;
+  }
   tcgen05_fence_before();
   __syncthreads();
   tcgen05_fence_after();
   const uint32_t tmem = misc->tmem_base;
+  const int kp = (a.d + 63) / 64, vp = (a.dv + 63) / 64;      // panels of 64 columns
+  const int total = (listed ? misc->live[a.B] : a.B * key_tiles) * a.Hk * gr.kv_pieces;
+  auto work_at = [&](int i) {
+    KvWork k;
+    int x = i;
+    k.piece = 0;
+    if (gr.kv_pieces > 1) { x = i / gr.kv_pieces; k.piece = i - x * gr.kv_pieces; }
+    int tile;
+    if (listed) {
+      k.b = 0;
+      for (int step = CROSS_RANKED / 2; step; step >>= 1)      // the last sequence that begins at x or before
+        if (k.b + step < a.B && misc->live[k.b + step] * a.Hk <= x) k.b += step;
+      const int own = misc->live[k.b + 1] - misc->live[k.b];
+      x -= misc->live[k.b] * a.Hk;
+      k.hk = x / own;
+      tile = x - k.hk * own;
+    } else {
+      k.unit = x / key_tiles;
+      tile = x - k.unit * key_tiles;
+      k.b = k.unit / a.Hk;
+      k.hk = k.unit - k.b * a.Hk;
+    }
+    k.unit = k.b * a.Hk + k.hk;
+    k.j0 = tile * TILE;
+    k.n = cross_keys(a, k.b);
+    k.t0 = 0;
+    k.items = row_tiles;
+    if (gr.kv_pieces > 1) {
+      k.t0 = (int)((int64_t)row_tiles * k.piece / gr.kv_pieces);
+      k.items = (int)((int64_t)row_tiles * (k.piece + 1) / gr.kv_pieces) - k.t0;
+    }
+    return k;
+  };
 
   if (warp >= CG_WARPS) regs_release<(Sm::BLOCKS == 2 ? CG_REGS_REST2 : CG_REGS_REST)>();
   if (warp == CGW_TMA) {
     if (lane == 0) {
-      int i = 0;
-      for (; i < items; i++) {
-        const int s = i % Sm::NS, h = hk * a.g + (t0 + i) / per, t = (t0 + i) % per;
-        const uint32_t parity = ((i / Sm::NS) & 1) ^ 1;
-        if (!mbar_wait(&misc->q_empty[s], parity, abortp, status)) break;
-        mbar_expect_tx(&misc->q_full[s], kp * Sm::PANEL + 8 * T);
-        for (int p = 0; p < kp; p++)
-          tma_load_4d(sm + Sm::Q + s * Sm::TILE_D + p * Sm::PANEL, &tmQ, &misc->q_full[s], p * 64, t * T, a.aq.sh ? h : 0, a.aq.sb ? b : 0);
-        const float* st = gr.stat + ((int64_t)b * a.H + h) * cross_stat_floats(a.Lq) + (int64_t)(t * T / 128) * 256 + t * T % 128;
-        bulk_load(sm + Sm::STAT + s * 8 * T, st, 4 * T, &misc->q_full[s]);
-        bulk_load(sm + Sm::STAT + s * 8 * T + 4 * T, st + 128, 4 * T, &misc->q_full[s]);
-        // (dY of a tile is done with before its Q is: its place is free by now, or the block has given up)
-        if (!mbar_wait(&misc->g_empty[s], parity, abortp, status)) { mbar_wait(&misc->q_full[s], (i / Sm::NS) & 1, abortp, status, false); break; }
-        mbar_expect_tx(&misc->g_full[s], vp * Sm::PANEL);
-        for (int p = 0; p < vp; p++)
-          tma_load_4d(sm + Sm::G + s * Sm::TILE_D + p * Sm::PANEL, &tmG, &misc->g_full[s], p * 64, t * T, gr.ady.sh ? h : 0, gr.ady.sb ? b : 0);
+      prefetch_tmap(&tmQ); prefetch_tmap(&tmG); prefetch_tmap(&tmK); prefetch_tmap(&tmV);
+      int at = 0, worked = 0;                          // tiles of rows and pieces of work so far
+      bool ok = true;
+      for (int wi = blockIdx.x; wi < total && ok; wi += gridDim.x, worked++) {
+        const KvWork k = work_at(wi);
+        if (!mbar_wait(&misc->kv_empty, (worked & 1) ^ 1, abortp, status)) break;
+        mbar_expect_tx(&misc->kv_full, (kp + vp) * TILE_BYTES);
+        for (int p = 0; p < kp; p++) tma_load_4d(sm + Sm::K + p * TILE_BYTES, &tmK, &misc->kv_full, p * 64, k.j0, a.ak.sh ? k.hk : 0, a.ak.sb ? k.b : 0);
+        for (int p = 0; p < vp; p++) tma_load_4d(sm + Sm::V + p * TILE_BYTES, &tmV, &misc->kv_full, p * 64, k.j0, a.av.sh ? k.hk : 0, a.av.sb ? k.b : 0);
+        int h = k.hk * a.g + k.t0 / per, t = k.t0 % per;
+        for (int i = 0; i < k.items; i++, at++) {
+          const int s = at % Sm::NS;
+          const uint32_t parity = ((at / Sm::NS) & 1) ^ 1;
+          // (dY of a tile is done with before its Q is)
+          if (!mbar_wait(&misc->q_empty[s], parity, abortp, status) || !mbar_wait(&misc->g_empty[s], parity, abortp, status)) { ok = false; break; }
+          mbar_expect_tx(&misc->q_full[s], kp * Sm::PANEL + 8 * T);
+          for (int p = 0; p < kp; p++)
+            tma_load_4d(sm + Sm::Q + s * Sm::TILE_D + p * Sm::PANEL, &tmQ, &misc->q_full[s], p * 64, t * T, a.aq.sh ? h : 0, a.aq.sb ? k.b : 0);
+          const float* st = gr.stat + ((int64_t)k.b * a.H + h) * cross_stat_floats(a.Lq) + (int64_t)(t * T / 128) * 256 + t * T % 128;
+          bulk_load(sm + Sm::STAT + s * 8 * T, st, 4 * T, &misc->q_full[s]);
+          bulk_load(sm + Sm::STAT + s * 8 * T + 4 * T, st + 128, 4 * T, &misc->q_full[s]);
+          mbar_expect_tx(&misc->g_full[s], vp * Sm::PANEL);
+          for (int p = 0; p < vp; p++)
+            tma_load_4d(sm + Sm::G + s * Sm::TILE_D + p * Sm::PANEL, &tmG, &misc->g_full[s], p * 64, t * T, gr.ady.sh ? h : 0, gr.ady.sb ? k.b : 0);
+          if (++t == per) { t = 0; h++; }
+        }
+        if (!ok) mbar_wait(&misc->kv_full, worked & 1, abortp, status, false);
       }
       // nothing of this block may still be in flight when it exits: no copy, and no arrival of a product's completion
-      mbar_wait(&misc->kv_full, 0, abortp, status, false);
-      for (int k = max(0, i - Sm::NS); k < i; k++) {
+      if (ok && worked > 0) {
+        mbar_wait(&misc->kv_full, (worked - 1) & 1, abortp, status, false);
+        mbar_wait(&misc->kv_empty, (worked - 1) & 1, abortp, status);
+      }
+      for (int k = max(0, at - Sm::NS); k < at; k++) {
         const uint32_t parity = (k / Sm::NS) & 1;
         mbar_wait(&misc->q_full[k % Sm::NS], parity, abortp, status, false);
         mbar_wait(&misc->g_full[k % Sm::NS], parity, abortp, status, false);
@@ -157,9 +207,9 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     const int ks = a.d / 16, vs = a.dv / 16;
     const bool leader = elect_one();
     auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, abortp, status); };
-    auto issue_s = [&](int i) {
-      const int s = i % Sm::NS;
-      if (!wait(&misc->q_full[s], (i / Sm::NS) & 1)) return false;
+    auto issue_s = [&](int at) {
+      const int s = at % Sm::NS;
+      if (!wait(&misc->q_full[s], (at / Sm::NS) & 1)) return false;
       tcgen05_fence_after();
       if (leader) {
         Desc q = q0;
@@ -170,111 +220,136 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       __syncwarp();
       return true;
     };
-    auto issue_dp = [&](int i) {
-      const int s = i % Sm::NS;
-      if (!wait(&misc->g_full[s], (i / Sm::NS) & 1)) return false;
+    auto issue_dp = [&](int at, bool last) {
+      const int s = at % Sm::NS;
+      if (!wait(&misc->g_full[s], (at / Sm::NS) & 1)) return false;
       tcgen05_fence_after();
       if (leader) {
         Desc g = g0;
         g.lo += s * (Sm::TILE_D / 16);
         issue_rows<D / 16, TILE_BYTES, Sm::PANEL>(tmem + Sm::P, v0, g, ID_S, vs);
+        if (last) mma_commit(&misc->kv_empty);
         mma_commit(&misc->dp_full);
       }
       __syncwarp();
       return true;
     };
-    bool ok = wait(&misc->kv_full, 0) && issue_s(0) && issue_dp(0);
-    for (int i = 0; i < items && ok; i++) {
-      const int s = i % Sm::NS;
-      if (!(ok = wait(&misc->p_ready, i & 1))) break;
-      tcgen05_fence_after();
-      if (leader) {
-        Desc g = gt;
-        g.lo += s * (Sm::TILE_D / 16);
-        issue_halves<T, T / 2>(tmem + Sm::DV, tmem + Sm::S, g, ID_V, i > 0);
-        mma_commit(&misc->g_empty[s]);
+    int at = 0, worked = 0;
+    bool ok = true;
+    for (int wi = blockIdx.x; wi < total && ok; wi += gridDim.x, worked++) {
+      const int items = work_at(wi).items;
+      ok = wait(&misc->kv_full, worked & 1) && issue_s(at) && issue_dp(at, items == 1);
+      for (int i = 0; i < items && ok; i++, at++) {
+        const int s = at % Sm::NS;
+        if (!(ok = wait(&misc->p_ready, at & 1))) break;
+        tcgen05_fence_after();
+        if (leader) {
+          Desc g = gt;
+          g.lo += s * (Sm::TILE_D / 16);
+          issue_halves<T, T / 2>(tmem + Sm::DV, tmem + Sm::S, g, ID_V, i > 0);
+          mma_commit(&misc->g_empty[s]);
+        }
+        __syncwarp();
+        if (i + 1 < items && !(ok = issue_s(at + 1))) break;
+        if (!(ok = wait(&misc->ds_ready, at & 1))) break;
+        tcgen05_fence_after();
+        if (leader) {
+          Desc q = qt;
+          q.lo += s * (Sm::TILE_D / 16);
+          issue_halves<T, T / 2>(tmem + Sm::DK, tmem + Sm::P, q, ID_K, i > 0);
+          mma_commit(&misc->q_empty[s]);
+          if (i == items - 1) mma_commit(&misc->done);
+        }
+        __syncwarp();
+        if (i + 1 < items) ok = issue_dp(at + 1, i + 2 == items);
       }
-      __syncwarp();
-      if (i + 1 < items && !(ok = issue_s(i + 1))) break;
-      if (!(ok = wait(&misc->ds_ready, i & 1))) break;
-      tcgen05_fence_after();
-      if (leader) {
-        Desc q = qt;
-        q.lo += s * (Sm::TILE_D / 16);
-        issue_halves<T, T / 2>(tmem + Sm::DK, tmem + Sm::P, q, ID_K, i > 0);
-        mma_commit(&misc->q_empty[s]);
-        if (i == items - 1) mma_commit(&misc->done);
-      }
-      __syncwarp();
-      if (i + 1 < items) ok = issue_dp(i + 1);
     }
   } else if (warp < CG_WARPS) {
     regs_acquire<(Sm::BLOCKS == 2 ? CG_REGS_ROWS2 : CG_REGS_ROWS)>();
-    const int w = warp >> 2, row = (warp & 3) * 32 + lane;      // w: which half of the tile's rows
+    const int w = warp >> 2, row = (warp & 3) * 32 + lane;      // w: which half of the tile's rows; and the first writes dV, the second dK
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), tS = lanes + Sm::S + w * (T / 2), tP = lanes + Sm::P + w * (T / 2);
     const float c = a.scale * FS_LOG2E;
-    bool ok = true;
-    for (int i = 0; i < items; i++) {
-      const int s = i % Sm::NS;
-      // (what a hidden key holds, NaNs too, stays in its own row of S^T, dP^T and of the sums, and is dropped at the end)
-      ok = __all_sync(0xffffffffu, mbar_wait(&misc->s_full, i & 1, abortp, status, false) &&
-                                       mbar_wait(&misc->q_full[s], (i / Sm::NS) & 1, abortp, status, false));
-      if (!ok) break;
-      tcgen05_fence_after();
-      const float* st = reinterpret_cast<const float*>(sm + Sm::STAT + s * 8 * T) + w * (T / 2);
-      uint32_t x[T / 2], g[T / 2];
-#pragma unroll
-      for (int q = 0; q < T / 32; q++) tmem_ld16(tS + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(x + 16 * q));
-      tmem_wait_ld();
-#pragma unroll
-      for (int q = 0; q < T / 2; q += 32) {
-        uint32_t o[16];
-#pragma unroll
-        for (int k = 0; k < 32; k += 4) {
-          const float4 nl = *reinterpret_cast<const float4*>(st + q + k);
-          uint32_t* xp = x + q + k;
-          fma2v(xp[0], xp[1], c, nl.x, nl.y);
-          fma2v(xp[2], xp[3], c, nl.z, nl.w);
-          exps2(xp[0], xp[1], false);
-          exps2(xp[2], xp[3], (k & 4) != 0);
-          o[k / 2] = pack_bf16(__uint_as_float(xp[0]), __uint_as_float(xp[1]));
-          o[k / 2 + 1] = pack_bf16(__uint_as_float(xp[2]), __uint_as_float(xp[3]));
-        }
-        tmem_st16(tS + q / 2, o);
+    // 16 values of a key's dV or dK, or of a piece's sums of them
+    auto store = [&](int unit, int b, int hk, int piece, int j, int q, const float (&x)[16]) {
+      const TensorAddr to = w ? gr.adk : gr.adv;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(w ? gr.dK : gr.dV) + b * to.sb + hk * to.sh + j * to.sl + q;
+      float* part = gr.pkv + (((int64_t)piece * a.B * a.Hk + unit) * a.Lk + j) * (a.d + a.dv) + (w ? 0 : a.d) + q;
+      store_row(j < a.Lk, x, gr.pkv ? part : nullptr, out);
+    };
+    const int width = w ? a.d : a.dv;
+    if (listed) {
+      const float none[16] = {};
+      for (int i = blockIdx.x; i < a.B * a.Hk * key_tiles; i += gridDim.x) {
+        const int unit = i / key_tiles, tile = i - unit * key_tiles, b = unit / a.Hk;
+        if (tile >= misc->live[b + 1] - misc->live[b])
+          for (int piece = 0; piece < gr.kv_pieces; piece++)
+            for (int q = 0; q < width; q += 16) store(unit, b, unit - b * a.Hk, piece, tile * TILE + row, q, none);
       }
-      tmem_wait_st();
-      tcgen05_fence_before();
-      mbar_arrive_warp(&misc->p_ready, lane);
-      ok = __all_sync(0xffffffffu, mbar_wait(&misc->dp_full, i & 1, abortp, status, false));
-      if (!ok) break;
-      tcgen05_fence_after();
-#pragma unroll
-      for (int q = 0; q < T / 32; q++) tmem_ld16(tP + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(g + 16 * q));
-      tmem_wait_ld();
-#pragma unroll
-      for (int q = 0; q < T / 2; q += 32) {
-        uint32_t u[16];
-#pragma unroll
-        for (int k = 0; k < 32; k += 4) {
-          const float4 nd = *reinterpret_cast<const float4*>(st + T + q + k);
-          uint32_t *xp = x + q + k, *gp = g + q + k;
-          addmul2(gp[0], gp[1], nd.x, nd.y, xp[0], xp[1]);
-          addmul2(gp[2], gp[3], nd.z, nd.w, xp[2], xp[3]);
-          u[k / 2] = pack_bf16(__uint_as_float(gp[0]), __uint_as_float(gp[1]));
-          u[k / 2 + 1] = pack_bf16(__uint_as_float(gp[2]), __uint_as_float(gp[3]));
-        }
-        tmem_st16(tP + q / 2, u);
-      }
-      tmem_wait_st();
-      tcgen05_fence_before();
-      mbar_arrive_warp(&misc->ds_ready, lane);
     }
-    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&misc->done, 0, abortp, status, false));
-    tcgen05_fence_after();
-    if (ok) {
-      // the first warpgroup writes dV, the second dK
-      const int j = j0 + row, width = w ? a.d : a.dv;
-      const bool on = cross_seen(a, b, j, n);
+    bool ok = true;
+    int at = 0, worked = 0;
+    for (int wi = blockIdx.x; wi < total; wi += gridDim.x, worked++) {
+      const KvWork k = work_at(wi);
+      for (int i = 0; i < k.items && ok; i++, at++) {
+        const int s = at % Sm::NS;
+        // (what a hidden key holds, NaNs too, stays in its own row of S^T, dP^T and of the sums, and is dropped at the end)
+        ok = __all_sync(0xffffffffu, mbar_wait(&misc->s_full, at & 1, abortp, status, false) &&
+                                         mbar_wait(&misc->q_full[s], (at / Sm::NS) & 1, abortp, status, false));
+        if (!ok) break;
+        tcgen05_fence_after();
+        const float* st = reinterpret_cast<const float*>(sm + Sm::STAT + s * 8 * T) + w * (T / 2);
+        uint32_t x[T / 2], g[T / 2];
+#pragma unroll
+        for (int q = 0; q < T / 32; q++) tmem_ld16(tS + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(x + 16 * q));
+        tmem_wait_ld();
+#pragma unroll
+        for (int q = 0; q < T / 2; q += 32) {
+          uint32_t o[16];
+#pragma unroll
+          for (int p = 0; p < 32; p += 4) {
+            const float4 nl = *reinterpret_cast<const float4*>(st + q + p);
+            uint32_t* xp = x + q + p;
+            fma2v(xp[0], xp[1], c, nl.x, nl.y);
+            fma2v(xp[2], xp[3], c, nl.z, nl.w);
+            exps2(xp[0], xp[1], false);
+            exps2(xp[2], xp[3], (p & 4) != 0);
+            o[p / 2] = pack_bf16(__uint_as_float(xp[0]), __uint_as_float(xp[1]));
+            o[p / 2 + 1] = pack_bf16(__uint_as_float(xp[2]), __uint_as_float(xp[3]));
+          }
+          tmem_st16(tS + q / 2, o);
+        }
+        tmem_wait_st();
+        tcgen05_fence_before();
+        mbar_arrive_warp(&misc->p_ready, lane);
+        ok = __all_sync(0xffffffffu, mbar_wait(&misc->dp_full, at & 1, abortp, status, false));
+        if (!ok) break;
+        tcgen05_fence_after();
+#pragma unroll
+        for (int q = 0; q < T / 32; q++) tmem_ld16(tP + 16 * q, *reinterpret_cast<uint32_t(*)[16]>(g + 16 * q));
+        tmem_wait_ld();
+#pragma unroll
+        for (int q = 0; q < T / 2; q += 32) {
+          uint32_t u[16];
+#pragma unroll
+          for (int p = 0; p < 32; p += 4) {
+            const float4 nd = *reinterpret_cast<const float4*>(st + T + q + p);
+            uint32_t *xp = x + q + p, *gp = g + q + p;
+            addmul2(gp[0], gp[1], nd.x, nd.y, xp[0], xp[1]);
+            addmul2(gp[2], gp[3], nd.z, nd.w, xp[2], xp[3]);
+            u[p / 2] = pack_bf16(__uint_as_float(gp[0]), __uint_as_float(gp[1]));
+            u[p / 2 + 1] = pack_bf16(__uint_as_float(gp[2]), __uint_as_float(gp[3]));
+          }
+          tmem_st16(tP + q / 2, u);
+        }
+        tmem_wait_st();
+        tcgen05_fence_before();
+        mbar_arrive_warp(&misc->ds_ready, lane);
+      }
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(&misc->done, worked & 1, abortp, status, false));
+      if (!ok) break;
+      tcgen05_fence_after();
+      const int j = k.j0 + row;
+      const bool on = cross_seen(a, k.b, j, k.n);
       const float f = w ? a.scale : 1.f;
       for (int q = 0; q < width; q += 16) {
         uint32_t t[16];
@@ -282,9 +357,10 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         tmem_wait_ld();
         float x[16];
 #pragma unroll
-        for (int k = 0; k < 16; k++) x[k] = on ? __uint_as_float(t[k]) * f : 0.f;
-        store(w, row, q, x);
+        for (int p = 0; p < 16; p++) x[p] = on ? __uint_as_float(t[p]) * f : 0.f;
+        store(k.unit, k.b, k.hk, k.piece, j, q, x);
       }
+      tcgen05_fence_before();                          // (the sums have been read before the next P and dS are handed over)
     }
   }
   tcgen05_fence_before();
@@ -544,8 +620,9 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 
 template <int D>
 int launch(fsharp_ctx* ctx, const CrossArgs& a, const CrossGrad& gr) {
-  const int64_t gk = ((int64_t)a.Lk + TILE - 1) / TILE * gr.kv_pieces, gq = ((int64_t)a.g * a.Lq + 255) / 256 * gr.q_pieces;
-  if (gk > 0x7fffffff || gq > 0x7fffffff) return FSHARP_E_SHAPE;
+  const int64_t keys = ((int64_t)a.Lk + TILE - 1) / TILE, works = keys * gr.kv_pieces * a.B * a.Hk, gq = ((int64_t)a.g * a.Lq + 255) / 256 * gr.q_pieces;
+  if (works > 0x7fff0000 || gq > 0x7fffffff) return FSHARP_E_SHAPE;
+  const int64_t resident = (int64_t)ctx->sm_count * KvSm<D>::BLOCKS;
   CUtensorMap tmQ, tmG, tmK, tmV, tmKt, tmVt;
   FS_TRY(fs_tc_cross_map(&tmQ, a.Q, a.aq, a.B, a.H, a.Lq, a.d, KvSm<D>::T));
   FS_TRY(fs_tc_cross_map(&tmG, gr.dY, gr.ady, a.B, a.H, a.Lq, a.dv, KvSm<D>::T));
@@ -556,7 +633,8 @@ int launch(fsharp_ctx* ctx, const CrossArgs& a, const CrossGrad& gr) {
   FS_CUDA_OK(fs_allow_smem(tc_cross_dkv_kernel<D>));
   FS_CUDA_OK(fs_allow_smem(tc_cross_dq_kernel<D>));
   FS_TIME_BEGIN(ctx, FS_K_TC_CROSS_DKV);
-  tc_cross_dkv_kernel<D><<<dim3((unsigned)gk, (unsigned)(a.B * a.Hk)), CG_T, KvSm<D>::TOTAL + 1024, ctx->stream>>>(tmQ, tmG, tmK, tmV, a, gr, ctx->d_status);
+  tc_cross_dkv_kernel<D><<<dim3((unsigned)(works < resident ? works : resident)), CG_T, KvSm<D>::TOTAL + 1024, ctx->stream>>>(
+      tmQ, tmG, tmK, tmV, a, gr, (int)keys, ctx->d_status);
   FS_TIME_END(ctx);
   FS_LAUNCH_CHECK(ctx);
   CrossArgs aq = a;
