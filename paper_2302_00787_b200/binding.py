@@ -5,6 +5,7 @@ or a call fails, an exception is raised."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import struct
 
@@ -216,8 +217,24 @@ def make_rope(rot, layout="half", base=10000.0, scaling="none", factor=1.0, orig
     return r
 
 
+def _on_its_stream(call):
+    """Runs a method with the context's stream as torch's current one: the copies of inputs that it makes, its scratch and
+    its new outputs are then ordered on the stream that its kernels run on, as the allocator expects."""
+    @functools.wraps(call)
+    def issue(self, *args, **named):
+        at = self._stream
+        if at is None or at == torch.cuda.current_stream(self.device).cuda_stream:
+            return call(self, *args, **named)
+        mine = torch.cuda.ExternalStream(at, self.device) if at else torch.cuda.default_stream(self.device)
+        with torch.cuda.stream(mine):
+            return call(self, *args, **named)
+    return issue
+
+
 class Context:
     """Owns one fsharp_ctx bound to a CUDA device and stream."""
+
+    _stream = None               # the stream's handle
 
     def __init__(self, device: int = 0, stream: torch.cuda.Stream | None = None):
         self.lib = load_library()
@@ -227,6 +244,7 @@ class Context:
         self._h = C.c_void_p()
         sp = stream.cuda_stream if stream is not None else torch.cuda.current_stream(device).cuda_stream
         _check(self.lib.fsharp_create(C.byref(self._h), device, C.c_void_p(sp)), "fsharp_create")
+        self._stream = sp
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -242,6 +260,7 @@ class Context:
     # -- plumbing
     def set_stream(self, stream: torch.cuda.Stream):
         _check(self.lib.fsharp_set_stream(self._h, C.c_void_p(stream.cuda_stream)), "fsharp_set_stream")
+        self._stream = stream.cuda_stream
 
     def set_impl(self, impl: int):
         _check(self.lib.fsharp_set_impl(self._h, impl), "fsharp_set_impl")
@@ -402,10 +421,11 @@ class Context:
             if t is not None and t.get_device() != self.device:
                 raise ValueError(f"{name}: expected a tensor on cuda:{self.device}, got {t.device}")
 
+    @_on_its_stream
     def fsharp_rotate(self, Q, K, rope, pos=None, pos0=0, transpose=False, out=None):
         """Rotary positions (make_rope) on Q [B,H,L,d] and K [B,Hk,L,d] (K may be None): (Q', K').  pos: int64 [B,L] or
         [L], None for 0 .. L-1; pos0 is added to it.  transpose: the gradient.  out: a pair of tensors to write, Q and K
-        themselves among them; the default is new dense ones."""
+        themselves among them; the default is new dense ones, of the context's stream."""
         here = self.device
         if Q.get_device() != here or (K is not None and K.get_device() != here) or (pos is not None and pos.get_device() != here):
             self._mine(Q=Q, K=K, pos=pos)
@@ -481,6 +501,7 @@ class Context:
         t = torch.empty(n, dtype=torch.uint8, device=device)
         return t, t.data_ptr(), n
 
+    @_on_its_stream
     def fsharp_cross_attend(self, Q, K, V, scale=None, key_len=None, key_mask=None, want_lse=False, out=None):
         """Exact softmax attention of Q [B,H,Lq,d] to K [B,Hk,Lk,d], V [B,Hk,Lk,dv]: Y, or (Y, lse [B,H,Lq] float32) with
         want_lse.  scale: d^-1/2 if None.  key_len: int32 [B].  key_mask: bool or uint8 [B,Lk] or [Lk], true where a key
@@ -506,6 +527,7 @@ class Context:
             raise FsharpError(rc, "fsharp_cross_attend")
         return (out, lse) if want_lse else out
 
+    @_on_its_stream
     def fsharp_cross_attend_backward(self, Q, K, V, Y, lse, dY, scale=None, key_len=None, key_mask=None):
         """(dQ, dK, dV) for the cotangent dY of fsharp_cross_attend's Y, with the Y and lse of that call; each gradient is a
         new tensor with its tensor's shape and, where those give every value a place of its own, its order of dimensions."""

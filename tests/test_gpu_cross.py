@@ -296,3 +296,87 @@ def test_offsets_past_32_bits(ctx):
         inside(Y, ref.Y, ref.bound_Y(BF16))
         for g, r, b in zip(ctx.fsharp_cross_attend_backward(Q, K, V, Y, lse, dY), ref.grads(dY), ref.bound_grads(dY, BF16)):
             inside(g, r, b)
+
+
+BATCHES = [
+    # B, H, Hk, Lq, Lk, d: several turns of every persistent block, sequences that are sorted by length or too many for it
+    (40, 8, 8, 130, 300, 64),
+    (24, 8, 4, 130, 300, 128),
+    (40, 12, 4, 43, 200, 32),
+    (260, 2, 2, 40, 70, 64),
+]
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16), ids=("f32", "bf16"))
+@pytest.mark.parametrize("kind", ("", "len", "bytes", "len+bytes"), ids=("full", "len", "bytes", "both"))
+@pytest.mark.parametrize("case", BATCHES, ids=["x".join(map(str, c)) for c in BATCHES])
+def test_more_tiles_than_blocks(ctx, case, kind, dtype):
+    B, H, Hk, Lq, Lk, d = case
+    gen = torch.Generator().manual_seed(11)
+    Q, K, V = (tensor(gen, B, *s, dtype, "blhd") for s in ((H, Lq, d), (Hk, Lk, d), (Hk, Lk, d)))
+    key_len = key_mask = None
+    if "len" in kind:
+        n = torch.randint(0, Lk + 1, (B,), generator=gen)
+        n[::7], n[3::11], n[-1] = 0, Lk, 1
+        key_len = n.int().cuda()
+    if "bytes" in kind:
+        key_mask = (torch.rand(B, Lk, generator=gen) < 0.5).cuda()
+        key_mask[5] = False
+    kw = {"scale": d ** -0.5, "key_len": key_len, "key_mask": key_mask}
+    ref = Cross(Q, K, V, d ** -0.5, key_len, key_mask)
+    K, V = spoil(K, ref.seen, gen), spoil(V, ref.seen, gen)
+    dY = tensor(gen, B, H, Lq, d, dtype, "blhd")
+    Y, lse = ctx.fsharp_cross_attend(Q, K, V, want_lse=True, **kw)
+    inside(Y, ref.Y, ref.bound_Y(dtype), "Y")
+    check_lse(lse, ref, d)
+    got = ctx.fsharp_cross_attend_backward(Q, K, V, Y, lse, dY, **kw)
+    for name, g, r, b in zip(("dQ", "dK", "dV"), got, ref.grads(dY), ref.bound_grads(dY, dtype)):
+        inside(g, r, b, name)
+    off = ~ref.seen[:, None].expand(-1, Hk, -1)
+    assert (got[1].cpu()[off] == 0).all() and (got[2].cpu()[off] == 0).all()
+    assert all(torch.equal(a, b) for a, b in zip(got, ctx.fsharp_cross_attend_backward(Q, K, V, Y, lse, dY, **kw)))
+    assert ctx.status() == 0
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16), ids=("f32", "bf16"))
+def test_keys_shared_by_all_heads(ctx, dtype):
+    """One key head stored once and broadcast over the heads; every head's gradient is its own."""
+    gen = torch.Generator().manual_seed(12)
+    Q, dY = (tensor(gen, 2, 4, 150, 64, dtype, "bhld") for _ in range(2))
+    K, V = (tensor(gen, 2, 1, 170, 64, dtype, "bhld").expand(2, 4, 170, 64) for _ in range(2))
+    ref = Cross(Q, K, V, 0.125)
+    Y, lse = ctx.fsharp_cross_attend(Q, K, V, want_lse=True)
+    inside(Y, ref.Y, ref.bound_Y(dtype))
+    for g, r, b in zip(ctx.fsharp_cross_attend_backward(Q, K, V, Y, lse, dY), ref.grads(dY), ref.bound_grads(dY, dtype)):
+        inside(g, r, b)
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16), ids=("f32", "bf16"))
+def test_context_on_another_stream(ctx, dtype):
+    """The current stream is busy: copies that a call makes of its inputs, and its scratch, belong to the context's stream."""
+    gen = torch.Generator().manual_seed(13)
+    Q, dY = (tensor(gen, 2, 4, 70, 64, dtype, "bhld") for _ in range(2))
+    K, V = (tensor(gen, 2, 4, 900, 66, dtype, "bhld")[..., 1:65] for _ in range(2))      # rows that have to be copied
+    rope = fb.make_rope(64)
+
+    def step(c):
+        Y, lse = c.fsharp_cross_attend(Q, K, V, want_lse=True)
+        return (Y,) + c.fsharp_cross_attend_backward(Q, K, V, Y, lse, dY) + c.fsharp_rotate(K, V, rope)
+    want = step(ctx)
+    side = torch.cuda.Stream()
+    mine = fb.Context(0, side)
+    for c in (mine, fb.Context(0)):                                  # (the second was made on the default stream)
+        c.set_stream(side)
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)
+        got = step(c)
+        side.synchronize()
+        with torch.cuda.stream(side):
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+        torch.cuda.synchronize()
+    with torch.cuda.stream(side):                                    # and back: the default stream's context, another one current
+        torch.cuda._sleep(20_000_000)
+        got = step(ctx)
+    torch.cuda.current_stream().synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    torch.cuda.synchronize()
