@@ -316,14 +316,17 @@ int fsharp_rotate(fsharp_ctx* ctx, const void* Q, const void* K, const int64_t* 
  * fsharp_cross_attend_backward writes, for a cotangent dY of Y, with D_i = dY_i . Y_i and dS = scale P (dY V^T - D):
  *   dQ = dS K,  dK = dS^T Q,  dV = P^T dY  (summed over the query heads that share a key head),
  * zero for rows that see nothing and for keys that are not seen.  Y and lse are those of the forward call.  All sums
- * are made in a fixed order: the same call gives the same bits.
+ * are made in a fixed order: the same call gives the same bits.  Lq = 0 with Lk > 0 is refused (FSHARP_E_SHAPE).
  *
  * scratch: device memory of at least fsharp_cross_scratch_bytes() bytes (16-byte aligned; may be NULL where that is 0),
  * used while the call's work is on the stream and not read before it is written.  It is the caller's, not the context's,
  * so that captured graphs and calls on several streams can each have their own; a graph keeps the pointer.
- * bf16 runs on the tensor cores (one query row per key head, forward: a multiply-add kernel that streams K and V), fp32 on
- * the multiply-add pipe in fp32 throughout.  FSHARP_IMPL_SIMT forces the multiply-add kernels;
- * FSHARP_IMPL_TENSOR refuses fp32 (FSHARP_E_SHAPE).  B * Hk <= 65535.  Strides of zero (one entry for a whole dimension)
+ * bf16 runs on the tensor cores (one query row per key head, forward: a multiply-add kernel that streams K and V).  fp32
+ * does too where d and dv are at most 64, with every operand as a sum of three bf16 numbers and the six products that
+ * fp32 can tell apart, sums in fp32: an infinity among seen values gives NaN there, and values below 2^-109 carry fewer
+ * bits.  fp32 with larger heads, and its forward pass with up to 16 query rows per key head, run on the multiply-add
+ * pipe.  FSHARP_IMPL_SIMT forces the multiply-add kernels; FSHARP_IMPL_TENSOR refuses fp32 with d or dv of 128
+ * (FSHARP_E_SHAPE).  B * Hk <= 65535.  Strides of zero (one entry for a whole dimension)
  * are allowed, but not for the tokens of K, V and, backward, Q and dY (FSHARP_E_SHAPE), and never in what is written. */
 typedef struct {
   int32_t B, H, Hk, Lq, Lk, d, dv;

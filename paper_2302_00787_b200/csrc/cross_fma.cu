@@ -1,4 +1,4 @@
-// Cross attention and its gradients on the multiply-add pipe, fp32 throughout: fp32 tensors (and bf16 ones where the tensor-core
+// Cross attention and its gradients on the multiply-add pipe, fp32 throughout: fp32 tensors of wide heads (and any where the tensor-core
 // kernels are not wanted).  Blocks of 256 threads; tiles of 64 keys and 16 or 64 rows lie row by row in shared memory as fp32,
 // every product is 4 x 4 (or 4 x D / 16) sums per thread with 16-byte loads of both operands: four loads of an operand row
 // serve 16 multiply-adds, which keeps the multiply-add pipe, not shared memory, the bound.

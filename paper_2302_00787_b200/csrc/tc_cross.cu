@@ -2,7 +2,7 @@
 //
 // A block has up to 256 rows of a unit (rows are packed over the query heads that share a key head) and walks the unit's keys
 // in tiles of 128.  Two warpgroups, thread = row: each has scores S (lanes: rows, columns: keys of tensor memory), from which its
-// threads read a row, take the maximum and the exponentials and put them back as bf16 P over S, and an output O that the
+// threads read a row, take the maximum and the exponentials and put them back as bf16 P (beside S or over it), and an output O that the
 // tensor core adds P V to from there.  Warps of their own copy K and V tiles (TMA, one ring, K before V) and issue the
 // products: S of the next tile and P V of one warpgroup run while the other one is at its exponentials.
 // With more than 128 rows the warpgroups take 128 rows each and share every K and V tile; with fewer they take the tiles in
