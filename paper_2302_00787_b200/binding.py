@@ -223,7 +223,7 @@ def _on_its_stream(call):
     @functools.wraps(call)
     def issue(self, *args, **named):
         at = self._stream
-        if at is None or at == torch.cuda.current_stream(self.device).cuda_stream:
+        if at is None or at == torch._C._cuda_getCurrentRawStream(self.device):      # (a Stream object: 2 us more per call)
             return call(self, *args, **named)
         mine = torch.cuda.ExternalStream(at, self.device) if at else torch.cuda.default_stream(self.device)
         with torch.cuda.stream(mine):
