@@ -316,7 +316,8 @@ int fsharp_rotate(fsharp_ctx* ctx, const void* Q, const void* K, const int64_t* 
  * fsharp_cross_attend_backward writes, for a cotangent dY of Y, with D_i = dY_i . Y_i and dS = scale P (dY V^T - D):
  *   dQ = dS K,  dK = dS^T Q,  dV = P^T dY  (summed over the query heads that share a key head),
  * zero for rows that see nothing and for keys that are not seen.  Y and lse are those of the forward call.  All sums
- * are made in a fixed order: the same call gives the same bits.  Lq = 0 with Lk > 0 is refused (FSHARP_E_SHAPE).
+ * are made in a fixed order: the same call gives the same bits.  No query (H = 0 or Lq = 0) with keys is
+ * refused (FSHARP_E_SHAPE).
  *
  * scratch: device memory of at least fsharp_cross_scratch_bytes() bytes (16-byte aligned; may be NULL where that is 0),
  * used while the call's work is on the stream and not read before it is written.  It is the caller's, not the context's,

@@ -242,8 +242,8 @@ int fsharp_cross_attend_backward(fsharp_ctx* ctx, const void* Q, const void* K, 
   FS_TRY(check(ctx, dims, dtype));
   if (!(scale >= 0.f) || !isfinite(scale)) return FSHARP_E_BADARG;
   if (dims->mask_stride < 0) return FSHARP_E_BADARG;
-  if ((int64_t)dims->B * dims->H == 0) return FSHARP_OK;
-  if (dims->Lq == 0) return dims->Lk == 0 ? FSHARP_OK : FSHARP_E_SHAPE;      // no query: nothing to differentiate
+  if ((int64_t)dims->B * dims->Hk == 0) return FSHARP_OK;
+  if (dims->H == 0 || dims->Lq == 0) return dims->Lk == 0 ? FSHARP_OK : FSHARP_E_SHAPE;      // no query: nothing to differentiate
   FS_TRY(check_tokens(Q, dtype, dims->q_stride, dims->Lq));
   FS_TRY(check_tensor(Y, dtype, dims->y_stride));
   FS_TRY(check_tokens(dY, dtype, dims->dy_stride, dims->Lq));

@@ -140,3 +140,9 @@ def test_binding_refuses_what_the_kernels_would_overrun(lib, blank):
     for y, s, g in ((x[:, :2], lse, x), (x, lse[:1], x), (x, lse.double(), x), (x, lse, x[..., :16])):
         with pytest.raises(ValueError):
             ctx.fsharp_cross_attend_backward(x, x, x, y, s, g)
+
+
+def test_no_query_with_keys_has_no_gradient(lib, blank):
+    """dK and dV would have to be written: the call must not report success and leave them as they were."""
+    assert cross(lib, blank, True, H=0) == SHAPE and cross(lib, blank, True, Lq=0) == SHAPE
+    assert cross(lib, blank, True, H=0, Lk=0) == 0 and cross(lib, blank, False, H=0) == 0
