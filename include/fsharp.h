@@ -284,7 +284,8 @@ int fsharp_kernel_apply(fsharp_ctx* ctx, const void* X, const void* Y, const voi
  * Q [B,H,L,d] and K [B,Hk,L,d] are turned by one launch (Hk = 0: queries alone, K and Kout may be NULL).
  * pos: device int64, position of token i of sequence b at pos[b * pos_stride + i] (pos_stride 0: shared by the batch);
  * NULL means i.  pos0 is added either way.  d in {16, 32, 64, 128}, rot even, 2 <= rot <= d.
- * Qout may be Q and Kout may be K (the same pointer and strides); outputs that overlap anything else are undefined. */
+ * Qout may be Q and Kout may be K (the same pointer and strides); outputs that overlap anything else are undefined,
+ * and refused where Qout is K, Kout is Q or Qout is Kout (FSHARP_E_BADARG). */
 enum { FSHARP_ROT_HALF = 0, FSHARP_ROT_INTERLEAVED = 1 };
 enum { FSHARP_ROPE_PLAIN = 0, FSHARP_ROPE_LINEAR = 1, FSHARP_ROPE_NTK = 2, FSHARP_ROPE_PARTS = 3 };
 typedef struct {
@@ -328,7 +329,8 @@ int fsharp_rotate(fsharp_ctx* ctx, const void* Q, const void* K, const int64_t* 
  * bits.  fp32 with larger heads, and its forward pass with up to 16 query rows per key head, run on the multiply-add
  * pipe.  FSHARP_IMPL_SIMT forces the multiply-add kernels; FSHARP_IMPL_TENSOR refuses fp32 with d or dv of 128
  * (FSHARP_E_SHAPE).  B * Hk <= 65535.  Strides of zero (one entry for a whole dimension)
- * are allowed, but not for the tokens of K, V and, backward, Q and dY (FSHARP_E_SHAPE), and never in what is written. */
+ * are allowed, but not for the tokens of K, V and, backward, Q and dY (FSHARP_E_SHAPE), and never in what is written.
+ * What is written (scratch too) may overlap no input and nothing else that is written. */
 typedef struct {
   int32_t B, H, Hk, Lq, Lk, d, dv;
   int64_t q_stride[3], k_stride[3], v_stride[3], y_stride[3];         /* element strides (batch, head, token) */

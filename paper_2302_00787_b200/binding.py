@@ -424,8 +424,8 @@ class Context:
     @_on_its_stream
     def fsharp_rotate(self, Q, K, rope, pos=None, pos0=0, transpose=False, out=None):
         """Rotary positions (make_rope) on Q [B,H,L,d] and K [B,Hk,L,d] (K may be None): (Q', K').  pos: int64 [B,L] or
-        [L], None for 0 .. L-1; pos0 is added to it.  transpose: the gradient.  out: a pair of tensors to write, Q and K
-        themselves among them; the default is new dense ones, of the context's stream."""
+        [L], None for 0 .. L-1; pos0 is added to it.  transpose: the gradient.  out: a pair of tensors to write, the first
+        may be Q and the second K (the other way round is refused); the default is new dense ones, of the context's stream."""
         here = self.device
         if Q.get_device() != here or (K is not None and K.get_device() != here) or (pos is not None and pos.get_device() != here):
             self._mine(Q=Q, K=K, pos=pos)

@@ -179,6 +179,8 @@ extern "C" int fsharp_rotate(fsharp_ctx* ctx, const void* Q, const void* K, cons
   const size_t es = dtype == FSHARP_F32 ? 4 : 2;
   if (dims->H) FS_TRY(check_side(Q, Qout, dims->q_stride, dims->qo_stride, es));
   if (dims->Hk) FS_TRY(check_side(K, Kout, dims->k_stride, dims->ko_stride, es));
+  // one tensor's output at the other's place: a thread would read what another has written
+  if (dims->H && dims->Hk && (Qout == K || Kout == Q || Qout == Kout)) return FSHARP_E_BADARG;
   FsDevice device(ctx->device);
   if (!device.ok) return FSHARP_E_CUDA;
 

@@ -146,3 +146,9 @@ def test_no_query_with_keys_has_no_gradient(lib, blank):
     """dK and dV would have to be written: the call must not report success and leave them as they were."""
     assert cross(lib, blank, True, H=0) == SHAPE and cross(lib, blank, True, Lq=0) == SHAPE
     assert cross(lib, blank, True, H=0, Lk=0) == 0 and cross(lib, blank, False, H=0) == 0
+
+
+def test_rotation_into_the_other_tensor(lib, blank):
+    for at in (dict(qo=2 * P, ko=P, q=P, k=2 * P), dict(qo=2 * P, ko=3 * P, q=P, k=2 * P), dict(qo=3 * P, ko=P, q=P, k=2 * P),
+               dict(qo=3 * P, ko=3 * P, q=P, k=2 * P)):
+        assert rotate(lib, blank, **at) == BADARG, at
