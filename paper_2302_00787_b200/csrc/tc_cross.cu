@@ -190,7 +190,8 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
           v.lo += vslot * (Sm::SLOT / 16);
           issue_cols<KT / 16>(tmem + w * Sm::GROUP + Sm::O, tmem + w * Sm::GROUP + Sm::P, v, ID_O, i > 1);
           if (!both || w) mma_commit(&misc->empty[vslot]);
-          mma_commit(&misc->o_full[w]);
+          // (OVER: the next S tells as much of the products before the last; a phase that nobody waits for is not completed)
+          if (!Sm::OVER || i + 2 >= items) mma_commit(&misc->o_full[w]);
         }
         __syncwarp();
         pn[w]++;
@@ -233,6 +234,7 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     };
     int done = 0;                                      // tiles of this warpgroup so far
     int ring = 0;                                      // copies of K and V so far
+    int outs = 0;                                      // OVER: pieces of work with tiles of this warpgroup so far
     bool ok = true;
     CxWork next = work_at(0);
     if (next.nt) fetch(next);
@@ -365,7 +367,7 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       if (place(round + 1) < total) next = work_at(round + 1);
       // (a warpgroup's own rows have been read when its last S is there; rows that both have read, only behind the barrier below)
       if (both && next.nt) fetch(next);
-      if (ok && mine > 0) ok = __all_sync(0xffffffffu, mbar_wait(&misc->o_full[w], (done - 1) & 1, abortp, status, false));
+      if (ok && mine > 0) ok = __all_sync(0xffffffffu, mbar_wait(&misc->o_full[w], (Sm::OVER ? outs++ : done - 1) & 1, abortp, status, false));
       tcgen05_fence_after();
       float sum = m == -INFINITY ? 0.f : __uint_as_float(l[0]) + __uint_as_float(l[1]);      // (2^-125 per hidden key from the cubic)
       const int h = k.hk * a.g + r / a.Lq, tok = r % a.Lq;
