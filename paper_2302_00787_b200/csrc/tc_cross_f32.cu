@@ -274,19 +274,9 @@ tc_cross_f32_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
       if (some) {
 #pragma unroll
         for (int q = 0; q < 2; q++) seen[q] = __ballot_sync(0xffffffffu, j0 + q * 32 + lane < n && look[q] != 0);
-        if (!both || w == 0) {
-          // what a hidden key's V holds may be anything: zeros in its place, a thread per key (one warpgroup does it for both: the
-          // other's product is issued behind its own)
-          const int slot = (2 * t + 1) % Sm::NS;
-          ok = __all_sync(0xffffffffu, mbar_wait(&misc->full[slot], ((2 * t + 1) / Sm::NS) & 1, abortp, status, false));
-          if (ok && row < KT && !(seen[warp & 1] >> lane & 1u))
-            for (int p = 0; p < 3; p++)
-              for (int k = 0; k < 8; k++) *reinterpret_cast<uint4*>(sm + Sm::RING + slot * SMALL3 + p * SMALL + row * 128 + k * 16) = make_uint4(0, 0, 0, 0);
-          fence_proxy_async_smem();
-        }
       }
       if (i + 1 < mine) peek(both ? i + 1 : 2 * i + 2 + w);
-      ok = ok && __all_sync(0xffffffffu, mbar_wait(&misc->s_full[w], i & 1, abortp, status, false));
+      ok = __all_sync(0xffffffffu, mbar_wait(&misc->s_full[w], i & 1, abortp, status, false));
       if (!ok) break;
       tcgen05_fence_after();
       uint32_t s[KT];
@@ -303,6 +293,18 @@ tc_cross_f32_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         if (!ok) break;
         tcgen05_fence_after();
         if (!idle) fold<64>(o, lanes + Sm::O, a.dv);
+      }
+      if (some && (!both || w == 0)) {
+        // What a hidden key's V holds may be anything: zeros in its place, a thread per key (one warpgroup does it for both: the
+        // other's product is issued behind its own).  Here, behind the product before, and not earlier: with tiles in turn the slot held
+        // this warpgroup's tile before, and until that one is known to have come, the wait below could be for its phase.
+        const int slot = (2 * t + 1) % Sm::NS;
+        ok = __all_sync(0xffffffffu, mbar_wait(&misc->full[slot], ((2 * t + 1) / Sm::NS) & 1, abortp, status, false));
+        if (!ok) break;
+        if (row < KT && !(seen[warp & 1] >> lane & 1u))
+          for (int p = 0; p < 3; p++)
+            for (int k = 0; k < 8; k++) *reinterpret_cast<uint4*>(sm + Sm::RING + slot * SMALL3 + p * SMALL + row * 128 + k * 16) = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
       }
       if (!idle) {
         if (some) {

@@ -380,3 +380,30 @@ def test_context_on_another_stream(ctx, dtype):
     torch.cuda.current_stream().synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16), ids=("f32", "bf16"))
+@pytest.mark.parametrize("kind", ("len", "bytes", "len+bytes"))
+@pytest.mark.parametrize("Lq,Lk,d", ((20, 1500, 64), (20, 1500, 32), (270, 1237, 64), (40, 1111, 128), (100, 2001, 64)))
+def test_few_rows_and_many_tiles(ctx, Lq, Lk, d, kind, dtype):
+    """Blocks of up to 128 rows, whose warpgroups take the tiles in turn, over many tiles in one piece, most of a block's warps
+    without rows: every tile's hidden keys are cleared in the tile itself.  The same bits in every run."""
+    B, H = 20, 8                                                     # (more units than SMs: one piece each)
+    gen = torch.Generator().manual_seed(14)
+    Q, K, V, dY = (tensor(gen, B, H, n, d, dtype, "blhd") for n in (Lq, Lk, Lk, Lq))
+    key_len = key_mask = None
+    if "len" in kind:
+        key_len = torch.randint(Lk // 2, Lk + 1, (B,), generator=gen).int().cuda()
+    if "bytes" in kind:
+        key_mask = (torch.rand(B, Lk, generator=gen) < 0.7).cuda()
+    kw = {"scale": d ** -0.5, "key_len": key_len, "key_mask": key_mask}
+    ref = Cross(Q, K, V, d ** -0.5, key_len, key_mask)
+    K, V = spoil(K, ref.seen, gen), spoil(V, ref.seen, gen)
+    runs = [ctx.fsharp_cross_attend(Q, K, V, want_lse=True, **kw) for _ in range(8)]
+    inside(runs[0][0], ref.Y, ref.bound_Y(dtype), "Y")
+    check_lse(runs[0][1], ref, d)
+    assert all(torch.equal(Y, runs[0][0]) and torch.equal(lse, runs[0][1]) for Y, lse in runs)
+    got = ctx.fsharp_cross_attend_backward(Q, K, V, *runs[0], dY, **kw)
+    for name, g, r, b in zip(("dQ", "dK", "dV"), got, ref.grads(dY), ref.bound_grads(dY, dtype)):
+        inside(g, r, b, name)
+    assert ctx.status() == 0
