@@ -10,8 +10,8 @@
 // O is only rescaled when a row's maximum has grown by more than 2^8 (l and O always have the same factor); P is then at most 2^8,
 // which bf16 holds as well as 1.
 // P is rounded to bf16 (2^-8 relative) as the tensor core's operand; l sums the exponentials before that rounding, in fp32.
-// Bound: exponentials (128 x 128 per tile and warpgroup at 16 per clock, one in eight by a cubic on the multiply-add pipe) and the
-// instructions around them.  4 x 12 x 4096 queries, 8192 keys, d = 64: 626 us, 658 TFLOP/s, at 1965 MHz and 940 W of 1000; without the
+// Bound: exponentials (128 x 128 per tile and warpgroup at 16 per clock, one in eight by a quartic on the multiply-add pipe) and the
+// instructions around them.  4 x 12 x 4096 queries, 8192 keys, d = 64: 624 us, 661 TFLOP/s, at 1965 MHz and 940 W of 1000; without the
 // warpgroups' arithmetic 441 us.  (Two threads per row, half of the keys each, 16 warps: 679 us; two blocks per SM with tiles of 64
 // keys: 726 us.)
 #include "cross.cuh"
@@ -309,7 +309,7 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             top = max3n(max3n(top, t1, t2), t3, t3);
           }
           top *= c;
-          // (an infinite score makes the row NaN as its definition does: the cubic below would drop inf - inf)
+          // (an infinite score makes the row NaN as its definition does: the quartic below would drop inf - inf)
           if (top == INFINITY) top = __uint_as_float(0x7fc00000u);
           const bool grown = !(top <= m + CX_SLACK) && top != -INFINITY;
           // the product that reads P and adds to O is done (OVER: S came behind it)
@@ -341,11 +341,11 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
 #pragma unroll
             for (int p = 0; p < 32; p += 2) {
               fma2(s[q + p], s[q + p + 1], c, base);
-              if ((p & 15) < 14) {                       // (one pair of eight by the cubic: 626 us; none 647, two 632, three 686)
+              if ((p & 15) < 14) {                       // (one pair of eight by the quartic: 624 us, as by a cubic; by a quintic 645, none 647, two cubics 632, three 686)
                 s[q + p] = __float_as_uint(ex2(__uint_as_float(s[q + p])));
                 s[q + p + 1] = __float_as_uint(ex2(__uint_as_float(s[q + p + 1])));
               } else {
-                exp2_poly2(s[q + p], s[q + p + 1]);
+                exp2_quartic2(s[q + p], s[q + p + 1]);
               }
               add2(l[0], l[1], __uint_as_float(s[q + p]), __uint_as_float(s[q + p + 1]));
               o[p / 2] = pack_bf16(__uint_as_float(s[q + p]), __uint_as_float(s[q + p + 1]));
@@ -369,7 +369,7 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       if (both && next.nt) fetch(next);
       if (ok && mine > 0) ok = __all_sync(0xffffffffu, mbar_wait(&misc->o_full[w], (Sm::OVER ? outs++ : done - 1) & 1, abortp, status, false));
       tcgen05_fence_after();
-      float sum = m == -INFINITY ? 0.f : __uint_as_float(l[0]) + __uint_as_float(l[1]);      // (2^-125 per hidden key from the cubic)
+      float sum = m == -INFINITY ? 0.f : __uint_as_float(l[0]) + __uint_as_float(l[1]);      // (2^-125 per hidden key from the quartic)
       const int h = k.hk * a.g + r / a.Lq, tok = r % a.Lq;
       const int64_t at = ((int64_t)k.unit * part.pieces + k.piece) * R + r;
       __nv_bfloat16* y = Y + b * ay.sb + h * ay.sh + tok * ay.sl;

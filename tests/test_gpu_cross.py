@@ -407,3 +407,14 @@ def test_few_rows_and_many_tiles(ctx, Lq, Lk, d, kind, dtype):
     for name, g, r, b in zip(("dQ", "dK", "dV"), got, ref.grads(dY), ref.bound_grads(dY, dtype)):
         inside(g, r, b, name)
     assert ctx.status() == 0
+
+
+@pytest.mark.parametrize("Lq,Lk,d", ((207, 31, 64), (300, 46, 64), (130, 1500, 64), (260, 700, 128), (50, 75, 32), (200, 3, 16)))
+def test_log_sum_exp_of_bf16_tensors_is_an_fp32_number(ctx, Lq, Lk, d):
+    """Off by the scores' error, the exponentials' 3e-6 at most, the sum's additions and the roundings of lse: nothing of bf16's."""
+    gen = torch.Generator().manual_seed(15)
+    Q, K, V = (tensor(gen, 2, 4, n, d, BF16, "bhld") for n in (Lq, Lk, Lk))
+    ref = Cross(Q, K, V, d ** -0.5)
+    _, lse = ctx.fsharp_cross_attend(Q, K, V, want_lse=True)
+    bound = ref.score_error(d).amax(3) + 4e-6 + Lk * 2.0 ** -24 + 2.0 ** -22 * (1 + ref.lse.abs())
+    assert ((lse.cpu().double() - ref.lse).abs() <= bound).all()
