@@ -34,9 +34,9 @@ __device__ __forceinline__ void load_tile(float* to, int width, At at) {
     *reinterpret_cast<float4*>(to + r * (D + 4) + e) = p ? widen4(p + e) : make_float4(0.f, 0.f, 0.f, 0.f);
   }
 }
-// acc[i][j] += sum_k A[ty + 16 i][k] B[tx + 16 j][k], k < K
-template <int MT, int NT, int K>
-__device__ __forceinline__ void dots(float (&acc)[MT][NT], const float* A, const float* B, int ld) {
+// acc[i][j] += sum_k A[ty + 16 i][k] B[tx + 16 j][k], k < K (a multiple of 16; not the tiles' D, which is the larger of d and dv)
+template <int MT, int NT>
+__device__ __forceinline__ void dots(float (&acc)[MT][NT], const float* A, const float* B, int ld, int K) {
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll 4
   for (int k = 0; k < K; k += 4) {
@@ -61,10 +61,31 @@ template <int D> __device__ __forceinline__ int col_of(int c) {
   const int tx = threadIdx.x & 15;
   return D == 32 ? 2 * tx + c : 4 * tx + (c & 3) + (c >> 2) * 64;
 }
-// acc[i][c] += sum_k A[ty + 16 i][k] B[k][col(c)], k < 64 (A with rows of FM_LP, B of D + 4)
+// acc[i][c] += sum_k A[ty + 16 i][k] B[k][col(c)], k < 64 (A with rows of FM_LP, B of D + 4).  D = 128: the upper columns only where
+// `width` has them.
 template <int MT, int D>
-__device__ __forceinline__ void add_rows(float (&acc)[MT][D / 16], const float* A, const float* B) {
+__device__ __forceinline__ void add_rows(float (&acc)[MT][D / 16], const float* A, const float* B, int width) {
   const int ty = threadIdx.x >> 4;
+  if constexpr (D == 128) {
+    if (width <= 64) {
+#pragma unroll 2
+      for (int k = 0; k < 64; k += 4) {
+        float x[MT][4];
+#pragma unroll
+        for (int i = 0; i < MT; i++) *reinterpret_cast<float4*>(x[i]) = *reinterpret_cast<const float4*>(A + (ty + 16 * i) * FM_LP + k);
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+          float y[4];
+          *reinterpret_cast<float4*>(y) = *reinterpret_cast<const float4*>(B + (k + q) * (D + 4) + col_of<D>(0));
+#pragma unroll
+          for (int i = 0; i < MT; i++)
+#pragma unroll
+            for (int c = 0; c < 4; c++) acc[i][c] = fmaf(x[i][q], y[c], acc[i][c]);
+        }
+      }
+      return;
+    }
+  }
 #pragma unroll 2
   for (int k = 0; k < 64; k += 4) {
     float x[MT][4];
@@ -116,7 +137,7 @@ cross_fma_kernel(const __grid_constant__ CrossArgs a, T* __restrict__ Y, TensorA
     if (threadIdx.x < FM_KEYS) seen[threadIdx.x] = cross_seen(a, b, j0 + threadIdx.x, n);
     __syncthreads();
     float s[MT][4] = {};
-    dots<MT, 4, D>(s, sq, sk, LD);
+    dots<MT, 4>(s, sq, sk, LD, a.d);
 #pragma unroll
     for (int i = 0; i < MT; i++) {
       float top = m[i];
@@ -140,7 +161,7 @@ cross_fma_kernel(const __grid_constant__ CrossArgs a, T* __restrict__ Y, TensorA
       for (int k = 0; k < D / 16; k++) o[i][k] *= corr;
     }
     __syncthreads();
-    add_rows<MT, D>(o, sp, sv);
+    add_rows<MT, D>(o, sp, sv, a.dv);
   }
 #pragma unroll
   for (int i = 0; i < MT; i++) {
@@ -171,14 +192,14 @@ cross_fma_kernel(const __grid_constant__ CrossArgs a, T* __restrict__ Y, TensorA
 // What both kernels make of a pair of tiles: P and dS of rows ty + 16 i and keys tx + 16 j.
 template <int D>
 __device__ __forceinline__ void p_ds(float (&p)[4][4], float (&ds)[4][4], const float* sq, const float* sg, const float* sk, const float* sv,
-                                     const float2* stat, const int* seen, float c, float scale) {
+                                     const float2* stat, const int* seen, float c, float scale, int d, int dv) {
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll
   for (int i = 0; i < 4; i++)
 #pragma unroll
     for (int j = 0; j < 4; j++) p[i][j] = ds[i][j] = 0.f;
-  dots<4, 4, D>(p, sq, sk, D + 4);
-  dots<4, 4, D>(ds, sg, sv, D + 4);
+  dots<4, 4>(p, sq, sk, D + 4, d);
+  dots<4, 4>(ds, sg, sv, D + 4, dv);
 #pragma unroll
   for (int i = 0; i < 4; i++) {
     const float2 st = stat[ty + 16 * i];
@@ -223,7 +244,7 @@ cross_dkv_kernel(const __grid_constant__ CrossArgs a, const __grid_constant__ Cr
     if (threadIdx.x < 64) stat[threadIdx.x] = stat_of(a, gr, b, hk, r0 + threadIdx.x);
     __syncthreads();
     float p[4][4], ds[4][4];
-    p_ds<D>(p, ds, sq, sg, sk, sv, stat, seen, c, a.scale);
+    p_ds<D>(p, ds, sq, sg, sk, sv, stat, seen, c, a.scale, a.d, a.dv);
 #pragma unroll
     for (int i = 0; i < 4; i++)
 #pragma unroll
@@ -232,8 +253,8 @@ cross_dkv_kernel(const __grid_constant__ CrossArgs a, const __grid_constant__ Cr
         sdt[(tx + 16 * j) * FM_LP + ty + 16 * i] = ds[i][j];
       }
     __syncthreads();
-    add_rows<4, D>(dv, spt, sg);
-    add_rows<4, D>(dk, sdt, sq);
+    add_rows<4, D>(dv, spt, sg, a.dv);
+    add_rows<4, D>(dk, sdt, sq, a.d);
   }
   __syncthreads();      // (seen, where no tile was walked)
 #pragma unroll
@@ -284,13 +305,13 @@ cross_dq_kernel(const __grid_constant__ CrossArgs a, const __grid_constant__ Cro
     load_tile<T, D, 64>(sv, a.dv, [&](int j) { return cross_seen(a, b, j0 + j, n) ? row_of<T>(a.V, a.av, b, hk, j0 + j) : nullptr; });
     __syncthreads();
     float p[4][4], ds[4][4];
-    p_ds<D>(p, ds, sq, sg, sk, sv, stat, seen, c, a.scale);
+    p_ds<D>(p, ds, sq, sg, sk, sv, stat, seen, c, a.scale, a.d, a.dv);
 #pragma unroll
     for (int i = 0; i < 4; i++)
 #pragma unroll
       for (int j = 0; j < 4; j++) sd[(ty + 16 * i) * FM_LP + tx + 16 * j] = ds[i][j];
     __syncthreads();
-    add_rows<4, D>(dq, sd, sk);
+    add_rows<4, D>(dq, sd, sk, a.d);
   }
 #pragma unroll
   for (int i = 0; i < 4; i++) {
