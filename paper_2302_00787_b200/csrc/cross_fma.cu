@@ -161,7 +161,13 @@ cross_fma_kernel(const __grid_constant__ CrossArgs a, T* __restrict__ Y, TensorA
       for (int k = 0; k < D / 16; k++) o[i][k] *= corr;
     }
     __syncthreads();
-    add_rows<MT, D>(o, sp, sv, a.dv);
+    // (a tile's sums on their own first: one sum over all keys is off by more, 1.1e-6 of the result instead of 3e-7 for 6127 keys)
+    float sum[MT][D / 16] = {};
+    add_rows<MT, D>(sum, sp, sv, a.dv);
+#pragma unroll
+    for (int i = 0; i < MT; i++)
+#pragma unroll
+      for (int k = 0; k < D / 16; k++) o[i][k] += sum[i][k];
   }
 #pragma unroll
   for (int i = 0; i < MT; i++) {
