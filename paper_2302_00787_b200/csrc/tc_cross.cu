@@ -345,7 +345,7 @@ tc_cross_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 s[q + p] = __float_as_uint(ex2(__uint_as_float(s[q + p])));
                 s[q + p + 1] = __float_as_uint(ex2(__uint_as_float(s[q + p + 1])));
               } else {
-                exp2_quartic2(s[q + p], s[q + p + 1]);
+                exp2_quartic2<false>(s[q + p], s[q + p + 1]);
               }
               add2(l[0], l[1], __uint_as_float(s[q + p]), __uint_as_float(s[q + p + 1]));
               o[p / 2] = pack_bf16(__uint_as_float(s[q + p]), __uint_as_float(s[q + p + 1]));

@@ -5,7 +5,12 @@
 
 namespace tcx {
 
-// max of three that hands NaNs on
+// max of two and of three that hands NaNs on
+__device__ __forceinline__ float max2n(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ float max3n(float a, float b, float c) {
   float r;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -36,8 +41,12 @@ __device__ __forceinline__ void addmul2(uint32_t& a, uint32_t& b, float n, float
 // (a, b) = 2^(a, b) on the multiply-add pipe: as exp2_poly2 of tc_common.cuh, with the quartic that exp2_poly_fit.py's fit(4) gives
 // (largest relative error 2.9e-6, 3.0e-6 with its sums in fp32): what a sum with one pair of eight from here is off by stays within
 // fp32's own errors, which the cubic's 8.6e-5 does not.  Arguments below -125 give 2^-125.
+// NANS: a NaN gives a NaN.  The bound below hands it on, and the power of two comes in by a product, which does too: added to the exponent's
+// field it would make a finite number of it.
+template <bool NANS>
 __device__ __forceinline__ void exp2_quartic2(uint32_t& a, uint32_t& b) {
-  const float x0 = fmaxf(__uint_as_float(a), -125.f), x1 = fmaxf(__uint_as_float(b), -125.f);
+  const float x0 = NANS ? max2n(__uint_as_float(a), -125.f) : fmaxf(__uint_as_float(a), -125.f);
+  const float x1 = NANS ? max2n(__uint_as_float(b), -125.f) : fmaxf(__uint_as_float(b), -125.f);
   uint32_t r0, r1, p0, p1;
   asm("{\n\t.reg .b64 x, r, n, f, p, c;\n\t"
       "mov.b64 x, {%4, %5};\n\t"
@@ -60,8 +69,16 @@ __device__ __forceinline__ void exp2_quartic2(uint32_t& a, uint32_t& b) {
       "mov.b64 {%2, %3}, p;\n\t}"
       : "=r"(r0), "=r"(r1), "=r"(p0), "=r"(p1)
       : "f"(x0), "f"(x1));
-  a = p0 + (r0 << 23);
-  b = p1 + (r1 << 23);
+  if constexpr (NANS) {
+    a = (r0 << 23) + 0x3f800000u;                      // 2^n: n in r's low bits
+    b = (r1 << 23) + 0x3f800000u;
+    asm("{\n\t.reg .b64 x, p;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 p, {%2, %3};\n\tmul.rn.f32x2 x, x, p;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+r"(a), "+r"(b)
+        : "r"(p0), "r"(p1));
+  } else {
+    a = p0 + (r0 << 23);
+    b = p1 + (r1 << 23);
+  }
 }
 
 // The products' issue.  One elected lane issues; what it takes to say a product (two descriptors, two addresses) has to be a

@@ -27,9 +27,10 @@ constexpr int HALF = 64;                                                // keys 
 constexpr uint32_t HALF_BYTES = 8192;                                   // 64 rows x 128 bytes
 constexpr uint32_t CG_DQ_TMEM = 512, CG_DQ_SUM = 256;                   // dq: two pairs (S, dP) of 64 columns each, then the two dQ
 
-// Two exponentials, by the special-function unit or by the cubic (one in four).
-__device__ __forceinline__ void exps2(uint32_t& x, uint32_t& y, bool cubic) {
-  if (cubic) exp2_poly2(x, y);
+// Two exponentials, by the special-function unit or by the quartic (one in four).  A NaN stays one: a NaN row of Q makes all of its P, and so
+// all of dV, NaN.
+__device__ __forceinline__ void exps2(uint32_t& x, uint32_t& y, bool quartic) {
+  if (quartic) exp2_quartic2<true>(x, y);
   else { x = __float_as_uint(ex2(__uint_as_float(x))); y = __float_as_uint(ex2(__uint_as_float(y))); }
 }
 

@@ -1,0 +1,86 @@
+"""NaNs and infinities among what the gradients of the exact cross attention see: a gradient is NaN where the definition in
+64 bits is, whatever the place of the bad row in a tile, and what does not depend on it stays as it was, bit for bit."""
+import math
+
+import pytest
+import torch
+
+from paper_2302_00787_b200 import binding as fb
+from tests.layer_util import Cross
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = fb.Context(0)
+    yield c
+    c.close()
+
+
+def gradients(ctx, Q, K, V, dY, **kw):
+    Y, lse = ctx.fsharp_cross_attend(Q, K, V, want_lse=True, **kw)
+    return (Y, lse) + ctx.fsharp_cross_attend_backward(Q, K, V, Y, lse, dY, **kw)
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16), ids=("f32", "bf16"))
+@pytest.mark.parametrize("impl", (fb.IMPL_AUTO, fb.IMPL_SIMT), ids=("auto", "simt"))
+@pytest.mark.parametrize("d,dv", ((64, 64), (128, 128), (32, 128)))
+@pytest.mark.parametrize("bad", (math.nan, math.inf, -math.inf))
+def test_bad_query_row_at_every_place(ctx, dtype, impl, d, dv, bad):
+    """One entry of one query row, at each place of eight neighbouring rows and of both halves of a tile."""
+    B, H, Hk, Lq, Lk = 2, 4, 2, 70, 150
+    gen = torch.Generator().manual_seed(0)
+    Q, dY = (torch.randn(B, H, Lq, n, generator=gen).to(dtype) for n in (d, dv))
+    K, V = (torch.randn(B, Hk, Lk, n, generator=gen).to(dtype) for n in (d, dv))
+    key_len = torch.tensor([Lk - 9, Lk], dtype=torch.int32)
+    ctx.set_impl(impl)
+    try:
+        clean = gradients(ctx, Q.cuda(), K.cuda(), V.cuda(), dY.cuda(), key_len=key_len.cuda())
+        for row in [*range(8), *range(30, 38), *range(62, 70)]:
+            q = Q.clone()
+            q[0, 1, row, 5] = bad
+            got = gradients(ctx, q.cuda(), K.cuda(), V.cuda(), dY.cuda(), key_len=key_len.cuda())
+            ref = Cross(q, K, V, d ** -0.5, key_len)
+            want = (ref.Y, None) + ref.grads(dY.double())
+            for name, g, c, r in zip(("Y", "lse", "dQ", "dK", "dV"), got, clean, want):
+                g, c = g.cpu(), c.cpu()
+                if r is not None:
+                    lost = torch.isnan(r) & ~torch.isnan(g)
+                    if name in ("dK", "dV"):
+                        lost &= ref.seen[:, None, :, None]          # (zeros at hidden keys, whatever else is NaN)
+                    assert not lost.any(), (name, row, int(lost.sum()))
+                # the bad row itself, and the keys that it shares with its key head, may be anything else
+                same = torch.ones_like(g, dtype=torch.bool)
+                if name in ("dK", "dV"):
+                    same[0, 0, : Lk - 9] = False
+                else:
+                    same[0, 1, row] = False
+                assert torch.equal(g[same], c[same]), (name, row)
+    finally:
+        ctx.set_impl(fb.IMPL_AUTO)
+    assert ctx.status() == 0
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16), ids=("f32", "bf16"))
+@pytest.mark.parametrize("d", (64, 128))
+def test_rows_of_nan_at_hidden_keys_and_of_empty_sequences(ctx, dtype, d):
+    """NaN queries and cotangents of a sequence without keys reach nobody; NaN cotangents of one head stay with its key head."""
+    B, H, Lq, Lk = 3, 2, 133, 140
+    gen = torch.Generator().manual_seed(1)
+    Q, K, V, dY = (torch.randn(B, H, n, d, generator=gen).to(dtype).cuda() for n in (Lq, Lk, Lk, Lq))
+    key_len = torch.tensor([Lk, 0, 77], dtype=torch.int32).cuda()
+    clean = gradients(ctx, Q, K, V, dY, key_len=key_len)
+    Q, dY = Q.clone(), dY.clone()
+    Q[1], dY[1], dY[2, 0] = math.nan, math.nan, math.nan
+    got = gradients(ctx, Q, K, V, dY, key_len=key_len)
+    for name, g, c in zip(("Y", "lse", "dQ", "dK", "dV"), got, clean):
+        same = torch.ones_like(g, dtype=torch.bool)
+        if name in ("dQ", "dK", "dV"):
+            same[2, 0] = False
+        assert torch.equal(g[same], c[same]), name
+    assert torch.isnan(got[2][2, 0]).all() and torch.isnan(got[3][2, 0, :77]).all() and torch.isnan(got[4][2, 0, :77]).all()
+    assert (got[3][2, 0, 77:] == 0).all() and (got[4][2, 0, 77:] == 0).all()
+    assert ctx.status() == 0
