@@ -197,6 +197,12 @@ def _written_place(t: torch.Tensor):
     return (b if B > 1 else H * L * inner, h if H > 1 else L * inner, l if L > 1 else inner)
 
 
+def _new_like(t: torch.Tensor) -> torch.Tensor:
+    """A new tensor of t's shape that the library can write: in t's order of dimensions where the last one is innermost, else dense."""
+    g = torch.empty_like(t)                                  # (permuted like a dense tensor, else dense)
+    return g if g.stride(3) == 1 else torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def make_dims(B, H, Lq, Lk, d, dv, M, pool=POOL_PER_BH, q=None, k=None, v=None, y=None,
               omega_head_stride=0) -> fsharp_dims:
     dm = fsharp_dims()
@@ -530,7 +536,8 @@ class Context:
     @_on_its_stream
     def fsharp_cross_attend_backward(self, Q, K, V, Y, lse, dY, scale=None, key_len=None, key_mask=None):
         """(dQ, dK, dV) for the cotangent dY of fsharp_cross_attend's Y, with the Y and lse of that call; each gradient is a
-        new tensor with its tensor's shape and, where those give every value a place of its own, its order of dimensions."""
+        new tensor with its tensor's shape and, where those give every value a place of its own and the last dimension is innermost,
+        its order of dimensions; otherwise (keys stored as [B,Hk,d,Lk], say) a dense one."""
         dt = _dtype_code(Q)
         sizes, len_at, mask_at, mask_stride = self._cross_check(Q, K, V, key_len, key_mask)
         self._mine(Y=Y, lse=lse, dY=dY)
@@ -540,7 +547,7 @@ class Context:
                 raise ValueError(f"{name}: expected {(B, H, Lq, dv)} of {Q.dtype}")
         if tuple(lse.shape) != (B, H, Lq) or lse.dtype != torch.float32 or not lse.is_contiguous():
             raise ValueError(f"lse: expected a contiguous float32 tensor of shape {(B, H, Lq)}")
-        dQ, dK, dV = torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V)      # (permuted like a dense tensor, else dense)
+        dQ, dK, dV = _new_like(Q), _new_like(K), _new_like(V)
         (Q, sq, q_at), (K, sk, k_at), (V, sv, v_at), (Y, sy, y_at), (dY, sg, g_at) = (_place(t) for t in (Q, K, V, Y, dY))
         dims = _CROSS_DIMS.pack(*sizes, *sq, *sk, *sv, *sy, *sg, *_written_place(dQ), *_written_place(dK), *_written_place(dV),
                                 mask_stride)
