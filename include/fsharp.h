@@ -280,7 +280,8 @@ int fsharp_kernel_apply(fsharp_ctx* ctx, const void* X, const void* Y, const voi
  *   PARTS   theta_j (keep + (1 - keep) / factor), keep = clamp((n - slow) / (fast - slow), 0, 1) with
  *           n = original theta_j / 2 pi the pair's turns in the trained length `original`
  * transpose != 0 applies the transposed map (t -> -t, gain kept): the gradient of the call, dX from dY.
- * Angles are formed in 64 bits (positions up to 2^31 in magnitude keep fp32's accuracy); each output is rounded once.
+ * Angles are formed in 64 bits and more (sine and cosine are off by less than 4 fp32 half steps of 1 at positions up to 2^31 in
+ * magnitude); each output is rounded once.
  * Q [B,H,L,d] and K [B,Hk,L,d] are turned by one launch (Hk = 0: queries alone, K and Kout may be NULL).
  * pos: device int64, position of token i of sequence b at pos[b * pos_stride + i] (pos_stride 0: shared by the batch);
  * NULL means i.  pos0 is added either way.  d in {16, 32, 64, 128}, rot even, 2 <= rot <= d.
