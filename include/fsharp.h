@@ -279,6 +279,7 @@ int fsharp_kernel_apply(fsharp_ctx* ctx, const void* X, const void* Y, const voi
  *   NTK     base factor^(rot / (rot - 2)) in place of base (rot > 2)
  *   PARTS   theta_j (keep + (1 - keep) / factor), keep = clamp((n - slow) / (fast - slow), 0, 1) with
  *           n = original theta_j / 2 pi the pair's turns in the trained length `original`
+ * A gain beyond fp32 and frequencies of more than 1e288 turns per position are refused (FSHARP_E_BADARG).
  * transpose != 0 applies the transposed map (t -> -t, gain kept): the gradient of the call, dX from dY.
  * Angles are formed in 64 bits and more (sine and cosine are off by less than 4 fp32 half steps of 1 at positions up to 2^31 in
  * magnitude); each output is rounded once.

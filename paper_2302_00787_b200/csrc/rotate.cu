@@ -171,7 +171,7 @@ extern "C" int fsharp_rotate(fsharp_ctx* ctx, const void* Q, const void* K, cons
   if (dtype != FSHARP_F32 && dtype != FSHARP_BF16) return FSHARP_E_DTYPE;
   if (rope->layout != FSHARP_ROT_HALF && rope->layout != FSHARP_ROT_INTERLEAVED) return FSHARP_E_BADARG;
   if (rope->scaling < FSHARP_ROPE_PLAIN || rope->scaling > FSHARP_ROPE_PARTS) return FSHARP_E_BADARG;
-  if (!positive(rope->base) || !isfinite(rope->gain)) return FSHARP_E_BADARG;
+  if (!positive(rope->base) || !isfinite((float)rope->gain)) return FSHARP_E_BADARG;
   if (rope->scaling != FSHARP_ROPE_PLAIN && !positive(rope->factor)) return FSHARP_E_BADARG;
   if (rope->scaling == FSHARP_ROPE_NTK && rot == 2) return FSHARP_E_SHAPE;     // one pair: the exponent rot / (rot - 2) has no value
   if (rope->scaling == FSHARP_ROPE_PARTS &&
@@ -185,16 +185,6 @@ extern "C" int fsharp_rotate(fsharp_ctx* ctx, const void* Q, const void* K, cons
   if (dims->Hk) FS_TRY(check_side(K, Kout, dims->k_stride, dims->ko_stride, es));
   // one tensor's output at the other's place: a thread would read what another has written
   if (dims->H && dims->Hk && (Qout == K || Kout == Q || Qout == Kout)) return FSHARP_E_BADARG;
-  FsDevice device(ctx->device);
-  if (!device.ok) return FSHARP_E_CUDA;
-
-  RotTensors t;
-  t.x[0] = Q; t.x[1] = K; t.y[0] = Qout; t.y[1] = Kout;
-  t.H[0] = dims->H; t.H[1] = dims->Hk;
-  t.ax[0] = fs_addr(dims->q_stride, dims->H, dims->L, d);
-  t.ax[1] = fs_addr(dims->k_stride, dims->Hk, dims->L, d);
-  t.ay[0] = fs_addr(dims->qo_stride, dims->H, dims->L, d);
-  t.ay[1] = fs_addr(dims->ko_stride, dims->Hk, dims->L, d);
   RotFreq f = {};
   const long double turn = 6.283185307179586476925286766559L, s = rope->factor;
   const long double base = rope->scaling == FSHARP_ROPE_NTK ? rope->base * powl(s, rot / (rot - 2.0L)) : (long double)rope->base;
@@ -207,9 +197,19 @@ extern "C" int fsharp_rotate(fsharp_ctx* ctx, const void* Q, const void* K, cons
       keep = keep < 0 ? 0 : keep > 1 ? 1 : keep;
       n = n / s * (1 - keep) + n * keep;
     }
+    if (!isfinite((double)(n * 0x1p64L))) return FSHARP_E_BADARG;      // (a position's turns would not be finite)
     f.turns[j] = (double)n;
     f.rest[j] = (double)(n - f.turns[j]);
   }
+  FsDevice device(ctx->device);
+  if (!device.ok) return FSHARP_E_CUDA;
+  RotTensors t;
+  t.x[0] = Q; t.x[1] = K; t.y[0] = Qout; t.y[1] = Kout;
+  t.H[0] = dims->H; t.H[1] = dims->Hk;
+  t.ax[0] = fs_addr(dims->q_stride, dims->H, dims->L, d);
+  t.ax[1] = fs_addr(dims->k_stride, dims->Hk, dims->L, d);
+  t.ay[0] = fs_addr(dims->qo_stride, dims->H, dims->L, d);
+  t.ay[1] = fs_addr(dims->ko_stride, dims->Hk, dims->L, d);
   // The widest vectors that rot / 2 is a multiple of: a thread's pairs then all turn or all pass, and the half layout's
   // second vector is aligned.
   const int half = rot / 2;
