@@ -582,14 +582,15 @@ tc_cross_f32_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     }
     const int j = j0 + row, width = w ? a.d : a.dv;
     if (ok && j < a.Lk) {
-      const float f = !cross_seen(a, b, j, n) ? 0.f : w ? a.scale : 1.f;
+      const float f = w ? a.scale : 1.f;
+      const bool on = cross_seen(a, b, j, n);
       const TensorAddr to = w ? gr.adk : gr.adv;
       float* out = gr.pkv ? gr.pkv + (((int64_t)piece * a.B * a.Hk + unit) * a.Lk + j) * (a.d + a.dv) + (w ? 0 : a.d)
                           : static_cast<float*>(w ? gr.dK : gr.dV) + b * to.sb + hk * to.sh + j * to.sl;
 #pragma unroll
       for (int k = 0; k < 64; k += 4)
         if (k < width)
-          *reinterpret_cast<float4*>(out + k) = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc[k] * f, acc[k + 1] * f, acc[k + 2] * f, acc[k + 3] * f);
+          *reinterpret_cast<float4*>(out + k) = on ? make_float4(acc[k] * f, acc[k + 1] * f, acc[k + 2] * f, acc[k + 3] * f) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     __syncwarp();
   }

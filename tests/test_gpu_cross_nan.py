@@ -84,3 +84,24 @@ def test_rows_of_nan_at_hidden_keys_and_of_empty_sequences(ctx, dtype, d):
     assert torch.isnan(got[2][2, 0]).all() and torch.isnan(got[3][2, 0, :77]).all() and torch.isnan(got[4][2, 0, :77]).all()
     assert (got[3][2, 0, 77:] == 0).all() and (got[4][2, 0, 77:] == 0).all()
     assert ctx.status() == 0
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16), ids=("f32", "bf16"))
+@pytest.mark.parametrize("impl", (fb.IMPL_AUTO, fb.IMPL_SIMT), ids=("auto", "simt"))
+@pytest.mark.parametrize("d", (64, 128))
+def test_scale_of_zero(ctx, dtype, impl, d):
+    """All scores are zero; dQ and dK are zero times their sums, NaN where those are."""
+    gen = torch.Generator().manual_seed(2)
+    Q, K, V, dY = (torch.randn(1, 2, n, d, generator=gen).to(dtype) for n in (70, 150, 150, 70))
+    Q[0, 0, 9, 3] = math.nan
+    ctx.set_impl(impl)
+    try:
+        got = gradients(ctx, Q.cuda(), K.cuda(), V.cuda(), dY.cuda(), scale=0.0)
+    finally:
+        ctx.set_impl(fb.IMPL_AUTO)
+    ref = Cross(Q, K, V, 0.0)
+    for name, g, r in zip(("Y", "dQ", "dK", "dV"), (got[0],) + got[2:], (ref.Y,) + ref.grads(dY.double())):
+        assert torch.equal(torch.isnan(g.cpu()), torch.isnan(r)), name
+        if name in ("dQ", "dK"):
+            assert (g.cpu()[~torch.isnan(r)] == 0).all(), name
+    assert ctx.status() == 0
