@@ -105,3 +105,32 @@ def test_scale_of_zero(ctx, dtype, impl, d):
         if name in ("dQ", "dK"):
             assert (g.cpu()[~torch.isnan(r)] == 0).all(), name
     assert ctx.status() == 0
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16), ids=("f32", "bf16"))
+@pytest.mark.parametrize("Lq", (1, 3))
+def test_as_many_units_as_there_may_be(ctx, dtype, Lq):
+    """B Hk = 65535, against the formulas in fp32 on the same device (sums over two keys and 16 features: 2e-6, and bf16's roundings)."""
+    B, Hk, g, Lk, d = 21845, 3, 2, 2, 16
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    Q, K, V, dY = (torch.randn(B, *s, d, generator=gen, device="cuda").to(dtype) for s in ((Hk * g, Lq), (Hk, Lk), (Hk, Lk), (Hk * g, Lq)))
+    key_len = torch.randint(0, Lk + 1, (B,), generator=gen, device="cuda").int()
+    got = gradients(ctx, Q, K, V, dY, key_len=key_len)
+    seen = (torch.arange(Lk, device="cuda") < key_len[:, None])[:, None, None]
+    q, k, v, y = Q.float(), K.float().repeat_interleave(g, 1), V.float().repeat_interleave(g, 1), dY.float()
+    S = (q @ k.transpose(2, 3) * d ** -0.5).masked_fill(~seen, -math.inf)
+    P = S.softmax(3).nan_to_num(0.0)
+    Y = P @ v
+    dS = P * (y @ v.transpose(2, 3) - (y * Y).sum(3, keepdim=True)) * d ** -0.5
+    fold = lambda t: t.unflatten(1, (Hk, g)).sum(2)                   # noqa: E731
+    want = (Y, S.logsumexp(3), dS @ k, fold(dS.transpose(2, 3) @ q), fold(P.transpose(2, 3) @ y))
+    for name, a, b in zip(("Y", "lse", "dQ", "dK", "dV"), got, want):
+        if name == "lse":
+            assert torch.equal(a == -math.inf, b == -math.inf)
+            assert (a - b)[b > -math.inf].abs().max() <= 1e-5
+        else:
+            # bf16: 0.0045 of dQ and dK by P, dS, Y (in D: all of dS where one key is seen) and the results rounded, made in 64 bits
+            assert torch.isfinite(a).all()
+            off, size = (a.float() - b).norm(), b.norm()
+            assert off <= (0.006 if dtype == BF16 else 4e-6) * size, (name, float(off / size))
+    assert ctx.status() == 0
