@@ -27,10 +27,10 @@ constexpr int HALF = 64;                                                // keys 
 constexpr uint32_t HALF_BYTES = 8192;                                   // 64 rows x 128 bytes
 constexpr uint32_t CG_DQ_TMEM = 512, CG_DQ_SUM = 256;                   // dq: two pairs (S, dP) of 64 columns each, then the two dQ
 
-// Two exponentials, by the special-function unit or by the quartic (one in four).  A NaN stays one: a NaN row of Q makes all of its P, and so
-// all of dV, NaN.
+// Two exponentials, by the special-function unit or by the quartic.  NANS: a NaN stays one.
+template <bool NANS>
 __device__ __forceinline__ void exps2(uint32_t& x, uint32_t& y, bool quartic) {
-  if (quartic) exp2_quartic2<true>(x, y);
+  if (quartic) exp2_quartic2<NANS>(x, y);
   else { x = __float_as_uint(ex2(__uint_as_float(x))); y = __float_as_uint(ex2(__uint_as_float(y))); }
 }
 
@@ -312,8 +312,10 @@ tc_cross_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             uint32_t* xp = x + q + p;
             fma2v(xp[0], xp[1], c, nl.x, nl.y);
             fma2v(xp[2], xp[3], c, nl.z, nl.w);
-            exps2(xp[0], xp[1], false);
-            exps2(xp[2], xp[3], (p & 4) != 0);
+            // a NaN row of Q makes all of its P, and so all of dV, NaN.  (One in eight by the quartic: 936 us for 4 x 12 x 4096 x 8192, d = 64; one
+            // in four 957, none 940; 271, 270 and 275 for 2 x 16 heads on 8, 2048 x 4096, d = 128)
+            exps2<true>(xp[0], xp[1], false);
+            exps2<true>(xp[2], xp[3], (p & 12) == 12);
             o[p / 2] = pack_bf16(__uint_as_float(xp[0]), __uint_as_float(xp[1]));
             o[p / 2 + 1] = pack_bf16(__uint_as_float(xp[2]), __uint_as_float(xp[3]));
           }
@@ -554,8 +556,10 @@ tc_cross_dq_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         for (int k = 0; k < 64; k += 4) {
           fma2(x[k], x[k + 1], c, st.x);
           fma2(x[k + 2], x[k + 3], c, st.x);
-          exps2(x[k], x[k + 1], false);
-          exps2(x[k + 2], x[k + 3], (k & 4) != 0);
+          // (a NaN of P needs no handing on here: D of its row is NaN.  One in four by the quartic: 884 us for 4 x 12 x 4096 x 8192, one in
+          // eight 902, none 917)
+          exps2<false>(x[k], x[k + 1], false);
+          exps2<false>(x[k + 2], x[k + 3], (k & 4) != 0);
           addmul2(g[k], g[k + 1], st.y, st.y, x[k], x[k + 1]);
           addmul2(g[k + 2], g[k + 3], st.y, st.y, x[k + 2], x[k + 3]);
         }
