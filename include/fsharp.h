@@ -313,7 +313,8 @@ int fsharp_rotate(fsharp_ctx* ctx, const void* Q, const void* K, const int64_t* 
  * key_len: device int32 [B], the keys of sequence b are 0 .. key_len[b] - 1 (values are clamped to 0 .. Lk); NULL: all Lk.
  * key_mask: device bytes, key j of sequence b is seen where key_mask[b * mask_stride + j] is not zero (mask_stride 0:
  * one mask for the batch); NULL: all.  Both may be given.  What K and V hold at keys that are not seen, NaNs and
- * infinities too, changes nothing.  A row that sees no key, or only scores of minus infinity, has Y = 0 and lse = -inf
+ * infinities too, changes nothing.  NaNs in seen keys and in queries come out as NaN in all that depends on them, and so may
+ * infinities (a score of plus infinity makes its row NaN).  A row that sees no key, or only scores of minus infinity, has Y = 0 and lse = -inf
  * (Lk = 0 is allowed).  lse: float32, dense [B,H,Lq], or NULL.
  *
  * fsharp_cross_attend_backward writes, for a cotangent dY of Y, with D_i = dY_i . Y_i and dS = scale P (dY V^T - D):

@@ -302,8 +302,17 @@ int run_join(fsharp_ctx* ctx, const CrossArgs& a, T* Y, TensorAddr ay, float* ls
 
 }  // namespace
 
-// Up to how many rows of a unit this kernel is the one to take: one of bf16 (more go to the tensor cores, which take up to 128 at the
-// price of one: 16 x 4 key heads, 16384 keys, d = 128: 182 us here and 165 there for one row, 249 and 90 for two), four of fp32.
+// Up to how many rows of a unit this kernel is the one to take: one of bf16, four of fp32.  Each call whole, us, by this kernel (with
+// its two- to eight-row forms of either type built for the measurement) for 1 | 2 | 4 | 8 rows, and by the other one, whose time hardly
+// depends on the rows up to 16:
+//                                     bf16, here          tensor cores    fp32, here              multiply-add tiles
+//   64 x 12 x 1500 keys, d = 64       70 | 70 | 88 | 191       100        115 | 115 | 131 | 195         594
+//   8 x 12 x 32768 keys, d = 64       174 | 182 | 223 | 408    207        301 | 317 | 365 | 537        1411
+//   32 x 8 x 1024 keys, d = 128       39 | 43 | 59 | 109       45         66 | 68 | 103 | 121           229
+//   16 x 4 x 16384 keys, d = 128      119 | 127 | 174 | 260    106        199 | 215 | 420 | 430         878
+//   1 x 8 x 512 keys, d = 64          8.2 | 10 | 10 | 16       14         12 | 12 | 12 | 14              16
+// So the rule is on the safe side: two bf16 rows of d = 64 and five to eight fp32 rows would still be faster here; one bf16 row against
+// long sequences of d = 128 would be 12 % faster on the tensor cores.
 int fs_cross_rows_most(int dtype) { return dtype == FSHARP_F32 ? 4 : 1; }
 
 // Pieces of the keys: enough for six blocks per SM, each with two turns of keys, where eight pieces (a cluster, which joins them

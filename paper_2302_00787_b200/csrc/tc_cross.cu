@@ -11,8 +11,8 @@
 // which bf16 holds as well as 1.
 // P is rounded to bf16 (2^-8 relative) as the tensor core's operand; l sums the exponentials before that rounding, in fp32.
 // Bound: exponentials (128 x 128 per tile and warpgroup at 16 per clock, one in eight by a quartic on the multiply-add pipe) and the
-// instructions around them.  4 x 12 x 4096 queries, 8192 keys, d = 64: 624 us, 661 TFLOP/s, at 1965 MHz and 940 W of 1000; without the
-// warpgroups' arithmetic 441 us.  (Two threads per row, half of the keys each, 16 warps: 679 us; two blocks per SM with tiles of 64
+// instructions around them.  4 x 12 x 4096 queries, 8192 keys, d = 64: 617 us, 669 TFLOP/s; without the warpgroups' arithmetic 459.
+// 16 heads on 4, 2049 x 10007, masked, d = 128: 181 us, without it 132.  (Two threads per row, half of the keys each, 16 warps: 679 us; two blocks per SM with tiles of 64
 // keys: 726 us.)
 #include "cross.cuh"
 #include "tc_common.cuh"

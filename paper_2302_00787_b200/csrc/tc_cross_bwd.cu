@@ -6,7 +6,8 @@
 // keep a fixed order.
 // Bound: the tensor pipe and, beside it, shared memory: a product with both operands there moves 128 bytes per clock where N = 128 and 192
 // where N = 64, its tiles' copies come on top; then the exponentials and the way from a product's end to the warps that wait for it
-// (without the warpgroups' arithmetic the two kernels of 2 x 16 heads on 8, 2048 x 4096, d = 128, take 219 us of 279 and 264 of 278).
+// (without the warpgroups' arithmetic the two kernels of 2 x 16 heads on 8, 2048 x 4096, d = 128, take 221 us of 267 and 219 of 224; of 16 x 12 x 512 x
+// 1500 ragged, d = 64, 93 of 112 and 73 of 84).
 #include "cross.cuh"
 #include "tc_common.cuh"
 #include "tc_cross.cuh"

@@ -858,6 +858,8 @@ struct Split {
 int parts_map(CUtensorMap* map, const __nv_bfloat16* parts, int BH, int L, int d, int rows) {
   return fs_tc_cross_map(map, parts, TensorAddr{(int64_t)BH * L * d, (int64_t)L * d, d}, 3, BH, L, d, rows);
 }
+// Pieces that bring `blocks` blocks up to one per SM (one is resident there), `most` at most: each has two tiles of keys forward, one of 128 rows or
+// keys backward.
 int pieces_for(const fsharp_ctx* ctx, int64_t blocks, int64_t most) {
   int64_t p = ctx->sm_count / blocks;
   if (p > most) p = most;
